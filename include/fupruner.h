@@ -82,7 +82,8 @@ typedef struct {
     int64_t bn_off;                     /* element offset into `bn` of this BN's 4*K values     */
 } fp_node;
 
-enum { FP_DTYPE_F32 = 0, FP_DTYPE_BF16 = 1 };
+enum { FP_DTYPE_F32 = 0, FP_DTYPE_BF16 = 1,
+       FP_DTYPE_F16 = 2 };          /* the training-step calls only (fp_linear_*, fp_cross_entropy, fp_adamw_step) */
 enum { FP_COMPUTE_BF16_TC = 0,     /* BF16 tensor-core path, fp32 accumulation (the product)   */
        FP_COMPUTE_FP32 = 1,        /* plain fp32 CUDA-core path, for validation only            */
        FP_COMPUTE_BF16_SIMT = 2 }; /* BF16 storage, CUDA-core convolutions: validation only     */
@@ -315,6 +316,157 @@ fp_status fp_soft_prune_finish(fp_handle h);
 #define FP_STATIC_RANK_MAX_FILTERS 4096
 fp_status fp_rank_filters_static(const float* d_filters, int32_t K, int32_t per_filter, int32_t norm, int32_t q,
                                  int32_t* d_rank, uint8_t* d_mask, void* stream);
+
+/* ---- the training step around pruning ------------------------------------------------------
+ *
+ * Algorithm 1 prunes between the epochs of a training loop ("update the parameters W by using data X", line 2).  These
+ * calls are that update for fully connected layers - the layer, its gradients, the loss they start from and the
+ * optimizer step over all tensors - so that a program can retrain a pruned network beside fp_score / fp_prune /
+ * fp_rank_filters_static without leaving the library.
+ *
+ * Conventions of these calls: they work on the caller's buffers and keep nothing; asynchronous on `stream` (NULL =
+ * default stream); no allocation and no host synchronisation, so that they can be captured into a CUDA graph; every
+ * buffer and the stream belong to the CURRENT device (FP_ERR_ARG for a buffer that is host memory or on another
+ * device).  Matrices are row major; ld_* is the number of ELEMENTS from one row to the next, at least the row's length;
+ * any alignment to the element's size is allowed.  Elements between a row's end and the next row are neither read
+ * into a result nor written.  Outputs may not overlap inputs or each other unless a call says so.
+ */
+
+enum { FP_ACT_NONE = 0, FP_ACT_RELU = 1,
+       FP_ACT_GELU = 2,             /* z Phi(z), Phi by erf                                                  */
+       FP_ACT_GELU_TANH = 3,        /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))                         */
+       FP_ACT_SILU = 4 };           /* z / (1 + e^-z)                                                        */
+
+typedef struct {
+    int64_t M, N, K;                /* rows (images, tokens), outputs, inputs; M >= 0, N, K >= 1             */
+    int32_t dtype;                  /* of x, w, res and pre: FP_DTYPE_BF16 or FP_DTYPE_F16                   */
+    int32_t y_dtype;                /* dtype or FP_DTYPE_F32                                                 */
+    int32_t bias_dtype;             /* dtype or FP_DTYPE_F32                                                 */
+    int32_t act;                    /* FP_ACT_*                                                              */
+    int32_t res_first;              /* 0: y = act(z) + res, z = x w' + bias.  1: z = x w' + bias + res,
+                                       y = act(z), a residual block's epilogue as in fp_forward              */
+    int32_t reserved;               /* 0                                                                     */
+    const void* d_x;                /* M x K                                                                 */
+    const void* d_w;                /* N x K                                                                 */
+    const void* d_bias;             /* N, or NULL                                                            */
+    const void* d_res;              /* M x N, or NULL.  May be d_y where y_dtype == dtype and ld_res == ld_y */
+    void* d_y;                      /* M x N out                                                             */
+    void* d_pre;                    /* M x N out: z, rounded to dtype - what fp_linear_backward takes; or NULL */
+    int64_t ld_x, ld_w, ld_res, ld_y, ld_pre;   /* of a buffer that is NULL: ignored                         */
+} fp_linear_args;
+
+/*
+ * fp_linear_forward - a fully connected layer: y = act(x w' + bias) + res (or act(x w' + bias + res)).
+ * Products are summed in 32 bits on the tensor cores; bias, activation and residual are applied to the 32-bit sum, which
+ * is rounded once.  What is not finite goes through by IEEE rules and stays in its row (x) or column (w, bias).
+ *   d_work, work_bytes   device scratch of at least fp_linear_workspace bytes, 256-byte aligned (NULL where that is 0).
+ *               Two calls that may run at the same time need two; so do two captured graphs that may.
+ * Errors: FP_ERR_ARG, FP_ERR_UNSUPPORTED (dtype), FP_ERR_BOUNDS (a size beyond 2^30, scratch too small), FP_ERR_CUDA.
+ */
+fp_status fp_linear_forward(const fp_linear_args* args, void* d_work, size_t work_bytes, void* stream);
+
+typedef struct {
+    int64_t M, N, K;                /* as in fp_linear_args; M == 0 gives dw = 0, db = 0                     */
+    int32_t dtype;                  /* of dy, x, w, pre, dx and dz: FP_DTYPE_BF16 or FP_DTYPE_F16            */
+    int32_t dw_dtype;               /* of dw and db: dtype or FP_DTYPE_F32                                   */
+    int32_t act;                    /* the layer's activation; pre is needed unless FP_ACT_NONE              */
+    int32_t accumulate;             /* 1: dw and db are added to what they hold (gradients of several batches) */
+    const void* d_dy;               /* M x N                                                                 */
+    const void* d_pre;              /* M x N, as fp_linear_forward wrote it                                  */
+    const void* d_x;                /* M x K; may be NULL where d_dw is                                      */
+    const void* d_w;                /* N x K; may be NULL where d_dx is                                      */
+    void* d_dx;                     /* M x K out, or NULL                                                    */
+    void* d_dw;                     /* N x K out, or NULL                                                    */
+    void* d_db;                     /* N out, or NULL                                                        */
+    void* d_dz;                     /* M x N out, or NULL: the gradient of z, which is that of res with res_first
+                                       (without, res has dy).  May be d_dy where ld_dz == ld_dy              */
+    int64_t ld_dy, ld_pre, ld_x, ld_w, ld_dx, ld_dw, ld_dz;
+} fp_linear_grad_args;
+
+/*
+ * fp_linear_backward - the gradients of fp_linear_forward:
+ *   dz = dy * act'(pre)      dx = dz w      dw = dz' x      db = sum of dz's rows
+ * dz is computed in 32 bits; db sums it unrounded, the two products take it rounded to dtype.  Sums are taken in 32 bits
+ * in an order that depends on the sizes alone: the same call gives the same bits.
+ * The derivative of relu at 0 is 0.  Scratch, streams and errors as in fp_linear_forward, with
+ * fp_linear_backward_workspace.  At least one output must be given.
+ */
+fp_status fp_linear_backward(const fp_linear_grad_args* args, void* d_work, size_t work_bytes, void* stream);
+
+/* Bytes of scratch that a call with these arguments needs (0 where every operand can be read in place: base address and
+ * row stride multiples of 16 bytes, and for fp_linear_backward no activation and no single dz).  Host only; depends on
+ * the sizes, the pointers' alignment and which pointers are NULL. */
+fp_status fp_linear_workspace(const fp_linear_args* args, size_t* bytes);
+fp_status fp_linear_backward_workspace(const fp_linear_grad_args* args, size_t* bytes);
+
+/* What a bounded device-side wait of fp_linear_forward / fp_linear_backward on the current device has met since the last
+ * call: FP_OK or FP_ERR_TIMEOUT (those results are invalid) in *h_status; synchronises with the device's work. */
+fp_status fp_linear_status(int32_t* h_status);
+
+typedef struct {
+    int64_t rows, classes;          /* rows >= 0, classes >= 1                                               */
+    int32_t dtype;                  /* of logits and dlogits: FP_DTYPE_F32, FP_DTYPE_BF16 or FP_DTYPE_F16    */
+    int32_t label_bytes;            /* 4: int32 labels, 8: int64                                             */
+    int64_t ignore_index;           /* rows with this label have loss 0 and gradient 0                       */
+    float label_smoothing;          /* e in [0, 1]: target = (1 - e) onehot + e / classes                    */
+    float grad_scale;               /* dlogits = grad_scale * row_grad * (softmax - target)                  */
+    const void* d_logits;           /* rows x classes                                                        */
+    const void* d_labels;           /* rows                                                                  */
+    const float* d_row_grad;        /* rows: the gradient of each row's loss, or NULL = 1                    */
+    float* d_loss;                  /* rows out, or NULL                                                     */
+    void* d_dlogits;                /* rows x classes out, or NULL.  May be d_logits where the strides agree */
+    int64_t ld_logits, ld_dlogits;
+} fp_cross_entropy_args;
+
+/*
+ * fp_cross_entropy - softmax cross-entropy of every row, loss = -sum target log softmax(logits), and its gradient, in
+ * one pass.  Sums and exponentials in 32 bits.  Logits of -inf have probability 0 (with smoothing they make the loss
+ * infinite, as the formula does); a row that is -inf throughout, or holds NaN or +inf, gives NaN in that row alone; so does a
+ * label outside [0, classes) other than ignore_index.  At least one of d_loss, d_dlogits.
+ * Errors: FP_ERR_ARG, FP_ERR_UNSUPPORTED (dtype), FP_ERR_BOUNDS (rows or classes beyond 2^30), FP_ERR_CUDA.
+ */
+fp_status fp_cross_entropy(const fp_cross_entropy_args* args, void* stream);
+
+#define FP_ADAMW_BLOCK 256          /* elements of a tensor that share one scale of an 8-bit state           */
+
+typedef struct {
+    int64_t n;                      /* elements, >= 0                                                        */
+    int64_t per_row;                /* elements a mask entry stands for (a filter's weights); ignored without d_mask */
+    int32_t p_dtype, g_dtype;       /* of the parameters and their gradient: FP_DTYPE_F32, _BF16 or _F16     */
+    int32_t state_bits;             /* 32 or 8                                                               */
+    int32_t reserved;               /* 0                                                                     */
+    void* d_p;                      /* updated in place                                                      */
+    const void* d_g;
+    void* d_m;                      /* first moment: float[n], or with state_bits 8 e4m3 codes, uint8[n]     */
+    void* d_v;                      /* second moment: float[n], or e4m3 codes of its SQUARE ROOT, uint8[n]   */
+    float* d_m_scale;               /* state_bits 8: float[ceil(n / FP_ADAMW_BLOCK)] each, value = code * scale */
+    float* d_v_scale;
+    const uint8_t* d_mask;          /* ceil(n / per_row) bytes, 1 keep / 0 pruned, e.g. from fp_rank_filters_static;
+                                       or NULL.  Pruned: p, m and v become 0, whatever the gradient is       */
+} fp_adamw_tensor;
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    double grad_scale;              /* gradients are multiplied by it first (1 / loss scale, clipping)       */
+    int64_t step;                   /* number of this step, from 1                                           */
+    const float* d_lr;              /* device scalars that are used instead where not NULL, read when the kernel */
+    const float* d_grad_scale;      /* runs: a captured step is replayed with the values they hold then      */
+    const int64_t* d_step;
+} fp_adamw_hyper;
+
+/*
+ * fp_adamw_step - one AdamW step (decoupled weight decay) over `count` tensors, a launch for each few hundred:
+ *   g' = grad_scale g   m = beta1 m + (1 - beta1) g'   v = beta2 v + (1 - beta2) g'^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ * in 32 bits, p rounded once to its type.  8-bit states are kept in blocks of 256 elements of a tensor: code =
+ * e4m3(x / scale), scale = largest |x| of the block / 448, rounded to nearest even; of v the square root is kept, which halves
+ * its exponent range, and a positive one never becomes 0 (it takes the smallest code), so that no
+ * step is divided by eps alone because of rounding.  The step itself uses m and v before they are rounded.
+ *   h_tensors   host; read before the call returns.  No two tensors may overlap.
+ * Errors: FP_ERR_ARG, FP_ERR_UNSUPPORTED (dtype, state_bits), FP_ERR_BOUNDS (n beyond 2^40), FP_ERR_CUDA; they are found
+ * before anything is launched, except FP_ERR_CUDA.
+ */
+fp_status fp_adamw_step(const fp_adamw_tensor* h_tensors, int32_t count, const fp_adamw_hyper* h_hyper, void* stream);
 
 /*
  * fp_debug_expire_wait - diagnostic (no counterpart in the paper): makes one bounded device-side wait run out on

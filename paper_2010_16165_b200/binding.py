@@ -17,16 +17,19 @@ _LIB_PATH = os.path.join(_HERE, "libfupruner.so")
 FP_OK = 0
 FP_ERR_ARG, FP_ERR_DESC, FP_ERR_SHAPE, FP_ERR_NONFINITE, FP_ERR_CUDA = -1, -2, -3, -4, -5
 FP_ERR_NOMEM, FP_ERR_UNSUPPORTED, FP_ERR_TIMEOUT, FP_ERR_EMPTY_LAYER, FP_ERR_BOUNDS = -6, -7, -8, -9, -10
-FP_DTYPE_F32, FP_DTYPE_BF16 = 0, 1
+FP_DTYPE_F32, FP_DTYPE_BF16, FP_DTYPE_F16 = 0, 1, 2
 FP_COMPUTE_BF16_TC, FP_COMPUTE_FP32, FP_COMPUTE_BF16_SIMT = 0, 1, 2
 FP_NORM_L1, FP_NORM_L2 = 0, 1
+FP_ACT_NONE, FP_ACT_RELU, FP_ACT_GELU, FP_ACT_GELU_TANH, FP_ACT_SILU = range(5)
+FP_ADAMW_BLOCK = 256
 (FP_Q_N_CONVS, FP_Q_CONV_K_FUSED, FP_Q_CONV_K_KEPT, FP_Q_CONV_C_KEPT, FP_Q_MASK, FP_Q_RANK, FP_Q_N_CLASSES,
  FP_Q_FLOPS, FP_Q_BYTES, FP_Q_N_OPS, FP_Q_OP_INFO, FP_Q_OP_OUTPUT, FP_Q_DEVICE_STATUS, FP_Q_N_LAUNCHES,
  FP_Q_OP_TIMES, FP_Q_CONV_BANK_ELEMS, FP_Q_ALL_MASKS, FP_Q_OP_PLAN) = range(18)
 
 EXPORTS = ["fp_fuse", "fp_prune", "fp_forward", "fp_forward_host", "fp_forward_host_async", "fp_score", "fp_query", "fp_destroy",
            "fp_last_error", "fp_rank_filters_static", "fp_soft_prune_epoch", "fp_soft_prune_finish",
-           "fp_debug_expire_wait", "fp_fuse_with_allocator"]
+           "fp_debug_expire_wait", "fp_fuse_with_allocator", "fp_linear_forward", "fp_linear_backward", "fp_linear_workspace",
+           "fp_linear_backward_workspace", "fp_linear_status", "fp_cross_entropy", "fp_adamw_step"]
 FP_STATIC_RANK_MAX_FILTERS = 4096
 OP_PLAN_FIELDS = ("tps", "cg", "groups", "groups2", "a_stages", "b_stages", "stays", "epi_warps", "alternate", "n_tile")
 CONV_KERNELS = ("", "conv_tc_kernel", "conv_split_kernel", "stem_pool_kernel", "chain_tc_kernel", "resident_net_kernel", "conv_simt_kernel",
@@ -53,6 +56,25 @@ class fp_op_info(ctypes.Structure):
                  "res_mode", "relu")] + \
                [("flops_per_image", ctypes.c_double), ("bytes_per_image", ctypes.c_double),
                 ("bytes_fixed", ctypes.c_double), ("chain", ctypes.c_int32), ("kernel", ctypes.c_int32)]
+
+
+def _struct(name, **fields):
+    """A ctypes structure from space-separated field names by type, in the order given."""
+    return type(name, (ctypes.Structure,), {"_fields_": [(f, t) for key, (t, names) in fields.items() for f in names.split()]})
+
+
+fp_linear_args = _struct("fp_linear_args", a=(ctypes.c_int64, "M N K"), b=(ctypes.c_int32, "dtype y_dtype bias_dtype act res_first reserved"),
+                         c=(ctypes.c_void_p, "d_x d_w d_bias d_res d_y d_pre"), d=(ctypes.c_int64, "ld_x ld_w ld_res ld_y ld_pre"))
+fp_linear_grad_args = _struct("fp_linear_grad_args", a=(ctypes.c_int64, "M N K"), b=(ctypes.c_int32, "dtype dw_dtype act accumulate"),
+                              c=(ctypes.c_void_p, "d_dy d_pre d_x d_w d_dx d_dw d_db d_dz"),
+                              d=(ctypes.c_int64, "ld_dy ld_pre ld_x ld_w ld_dx ld_dw ld_dz"))
+fp_cross_entropy_args = _struct("fp_cross_entropy_args", a=(ctypes.c_int64, "rows classes"), b=(ctypes.c_int32, "dtype label_bytes"),
+                                c=(ctypes.c_int64, "ignore_index"), d=(ctypes.c_float, "label_smoothing grad_scale"),
+                                e=(ctypes.c_void_p, "d_logits d_labels d_row_grad d_loss d_dlogits"), f=(ctypes.c_int64, "ld_logits ld_dlogits"))
+fp_adamw_tensor = _struct("fp_adamw_tensor", a=(ctypes.c_int64, "n per_row"), b=(ctypes.c_int32, "p_dtype g_dtype state_bits reserved"),
+                          c=(ctypes.c_void_p, "d_p d_g d_m d_v d_m_scale d_v_scale d_mask"))
+fp_adamw_hyper = _struct("fp_adamw_hyper", a=(ctypes.c_double, "lr beta1 beta2 eps weight_decay grad_scale"), b=(ctypes.c_int64, "step"),
+                         c=(ctypes.c_void_p, "d_lr d_grad_scale d_step"))
 
 
 ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p)
@@ -119,6 +141,13 @@ def lib():
         L.fp_debug_expire_wait.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
         L.fp_rank_filters_static.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                              ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+        for f in ("fp_linear_forward", "fp_linear_backward"):
+            getattr(L, f).argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        for f in ("fp_linear_workspace", "fp_linear_backward_workspace"):
+            getattr(L, f).argtypes = [ctypes.c_void_p, ctypes.POINTER(ctypes.c_size_t)]
+        L.fp_linear_status.argtypes = [ctypes.POINTER(ctypes.c_int32)]
+        L.fp_cross_entropy.argtypes = [ctypes.c_void_p, ctypes.c_void_p]
+        L.fp_adamw_step.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p]
         _lib = L
     return _lib
 
@@ -278,3 +307,180 @@ def masks_and_ranks(h):
 
 def op_infos(h):
     return [fp_query_op(h, i) for i in range(fp_query_int(h, FP_Q_N_OPS))]
+
+
+# ---- the training step around pruning (see the header's section of that name) ----------------------------------------
+
+_dtype_codes = None
+
+
+def _dtypes():
+    global _dtype_codes
+    if _dtype_codes is None:
+        import torch
+        _dtype_codes = {torch.float32: FP_DTYPE_F32, torch.bfloat16: FP_DTYPE_BF16, torch.float16: FP_DTYPE_F16}
+    return _dtype_codes
+
+
+def _dtype(t, name, want=None):
+    code = _dtypes().get(t.dtype)
+    if code is None or (want is not None and code not in want):
+        raise ValueError(f"{name} has dtype {t.dtype}")
+    return code
+
+
+def _matrix(t, rows, cols, name, dtype=None):
+    """(address, row stride) of a rows x cols tensor whose rows are contiguous; (None, 0) of None."""
+    if t is None:
+        return None, 0
+    if t.shape != (rows, cols) or not t.is_cuda or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype} on {t.device}: a CUDA tensor of {(rows, cols)}, {dtype} is wanted")
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"{name}: neighbours of a row must be neighbours in memory (strides {t.stride()})")
+    return t.data_ptr(), ld
+
+
+def _vector(t, n, name, dtype=None):
+    """Address of a contiguous vector of n elements; None of None."""
+    if t is None:
+        return None
+    if t.shape != (n,) or not t.is_cuda or (dtype is not None and t.dtype != dtype) or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype} on {t.device}: a contiguous CUDA vector of {n}, {dtype} is wanted")
+    return t.data_ptr()
+
+
+def _scratch(work):
+    return (None, 0) if work is None else (work.data_ptr(), work.numel() * work.element_size())
+
+
+def _linear_args(x, w, y, bias, res, pre, act, res_first):
+    (M, K), N, dt = x.shape, w.shape[0], x.dtype
+    px, lx = _matrix(x, M, K, "x")
+    pw, lw = _matrix(w, N, K, "w", dt)
+    py, ly = _matrix(y, M, N, "y")
+    pr, lr = _matrix(res, M, N, "res", dt)
+    pp, lp = _matrix(pre, M, N, "pre", dt)
+    return fp_linear_args(M, N, K, _dtype(x, "x"), _dtype(y, "y"), 0 if bias is None else _dtype(bias, "bias"), act, 1 if res_first else 0, 0,
+                          px, pw, _vector(bias, N, "bias"), pr, py, pp, lx, lw, lr, ly, lp)
+
+
+def fp_linear_forward(x, w, y, bias=None, res=None, pre=None, act=FP_ACT_NONE, res_first=False, work=None, stream=None):
+    """y = act(x w' + bias) + res, or act(x w' + bias + res) with res_first.  x (M, K), w (N, K), res and pre (M, N): bf16 or
+    f16 CUDA tensors with contiguous rows; y and bias: the same type or float32.  pre receives what the activation is taken of.
+    work: uint8 tensor of at least fp_linear_workspace bytes, or None where that is 0."""
+    a = _linear_args(x, w, y, bias, res, pre, act, res_first)
+    p, n = _scratch(work)
+    _check(lib().fp_linear_forward(ctypes.addressof(a), p, n, stream.cuda_stream if stream is not None else None))
+
+
+def fp_linear_workspace(x, w, y, bias=None, res=None, pre=None, act=FP_ACT_NONE, res_first=False):
+    """Bytes of scratch that fp_linear_forward needs for these tensors."""
+    a, n = _linear_args(x, w, y, bias, res, pre, act, res_first), ctypes.c_size_t()
+    _check(lib().fp_linear_workspace(ctypes.addressof(a), ctypes.byref(n)))
+    return n.value
+
+
+def _linear_grad_args(dy, x, w, dx, dw, db, dz, pre, act, accumulate):
+    M, N = dy.shape
+    K, dt = next((t.shape[1] for t in (x, w, dx, dw) if t is not None), 1), dy.dtype
+    pdy, ldy = _matrix(dy, M, N, "dy")
+    px, lx = _matrix(x, M, K, "x", dt)
+    pw, lw = _matrix(w, N, K, "w", dt)
+    pdx, ldx = _matrix(dx, M, K, "dx", dt)
+    pdw, ldw = _matrix(dw, N, K, "dw")
+    pdz, ldz = _matrix(dz, M, N, "dz", dt)
+    pp, lp = _matrix(pre, M, N, "pre", dt)
+    out = dw if dw is not None else db
+    code = _dtype(out, "dw") if out is not None else _dtype(dy, "dy")
+    return fp_linear_grad_args(M, N, K, _dtype(dy, "dy"), code, act, 1 if accumulate else 0, pdy, pp, px, pw, pdx, pdw,
+                               _vector(db, N, "db", None if out is None else out.dtype), pdz, ldy, lp, lx, lw, ldx, ldw, ldz)
+
+
+def fp_linear_backward(dy, x, w, dx=None, dw=None, db=None, dz=None, pre=None, act=FP_ACT_NONE, accumulate=False, work=None, stream=None):
+    """Gradients of fp_linear_forward, each where a tensor is given for it: dz = dy * act'(pre), dx = dz w, dw = dz' x, db = sum of
+    dz's rows (added to dw and db with accumulate).  x may be None without dw, w without dx.  dw and db: the inputs' type or
+    float32, both the same.  work: at least fp_linear_backward_workspace bytes, or None where that is 0."""
+    a = _linear_grad_args(dy, x, w, dx, dw, db, dz, pre, act, accumulate)
+    p, n = _scratch(work)
+    _check(lib().fp_linear_backward(ctypes.addressof(a), p, n, stream.cuda_stream if stream is not None else None))
+
+
+def fp_linear_backward_workspace(dy, x, w, dx=None, dw=None, db=None, dz=None, pre=None, act=FP_ACT_NONE, accumulate=False):
+    """Bytes of scratch that fp_linear_backward needs for these tensors."""
+    a, n = _linear_grad_args(dy, x, w, dx, dw, db, dz, pre, act, accumulate), ctypes.c_size_t()
+    _check(lib().fp_linear_backward_workspace(ctypes.addressof(a), ctypes.byref(n)))
+    return n.value
+
+
+def fp_linear_status():
+    """FP_OK, or FP_ERR_TIMEOUT where a device-side wait of the layers' kernels ran out since the last call (synchronises)."""
+    v = ctypes.c_int32()
+    _check(lib().fp_linear_status(ctypes.byref(v)))
+    return v.value
+
+
+def fp_cross_entropy(logits, labels, loss=None, dlogits=None, row_grad=None, label_smoothing=0.0, ignore_index=-100, grad_scale=1.0, stream=None):
+    """Softmax cross-entropy of every row of logits (rows, classes) with int32 or int64 labels (rows): loss (rows, float32) and dlogits
+    = grad_scale * row_grad * d loss / d logits, of the logits' type (it may be the logits themselves); either may be None."""
+    rows, classes = logits.shape
+    px, lx = _matrix(logits, rows, classes, "logits")
+    pd, ld = _matrix(dlogits, rows, classes, "dlogits", logits.dtype)
+    size = labels.element_size()
+    if labels.is_floating_point() or labels.is_complex() or size not in (4, 8) or str(labels.dtype)[6] == "u":
+        raise ValueError(f"labels have dtype {labels.dtype}")
+    f32 = next(k for k, v in _dtypes().items() if v == FP_DTYPE_F32)
+    a = fp_cross_entropy_args(rows, classes, _dtype(logits, "logits"), size, ignore_index, label_smoothing, grad_scale, px,
+                              _vector(labels, rows, "labels"), _vector(row_grad, rows, "row_grad", f32), _vector(loss, rows, "loss", f32), pd, lx, ld)
+    _check(lib().fp_cross_entropy(ctypes.addressof(a), stream.cuda_stream if stream is not None else None))
+
+
+class AdamwTensors:
+    """The table of a network's tensors for fp_adamw_step; holds the tensors, whose addresses it has."""
+
+    def __init__(self, array, tensors):
+        self.array, self.tensors = array, tensors
+
+
+def fp_adamw_tensors(tensors):
+    """tensors: dicts of CUDA tensors - p (float32, bf16 or f16; updated), g, m, v (float32 like p's shape, or e4m3 codes: float8_e4m3fn
+    or uint8 with float32 m_scale and v_scale, one for every FP_ADAMW_BLOCK elements) and optionally mask (uint8, one for every row of p,
+    or for every len / mask elements of a vector).  All contiguous.  Returns the table that fp_adamw_step takes."""
+    import torch
+    f8 = (torch.uint8, torch.float8_e4m3fn)
+    arr = (fp_adamw_tensor * len(tensors))()
+    for a, t in zip(arr, tensors):
+        p, g, m, v, mask = t["p"], t["g"], t["m"], t["v"], t.get("mask")
+        n, bits = p.numel(), 8 if m.dtype in f8 else 32
+        blocks = -(-n // FP_ADAMW_BLOCK)
+        for k, x in t.items():
+            if x is not None and (not x.is_cuda or not x.is_contiguous()):
+                raise ValueError(f"{k}: a contiguous CUDA tensor is wanted")
+        if g.numel() != n or m.numel() != n or v.numel() != n or m.dtype not in (f8 if bits == 8 else (torch.float32,)) or v.dtype != m.dtype:
+            raise ValueError("p, g, m and v must have one size, m and v one type (float32, or e4m3 codes)")
+        if bits == 8 and any(t[k].dtype != torch.float32 or t[k].numel() != blocks for k in ("m_scale", "v_scale")):
+            raise ValueError(f"m_scale and v_scale must be {blocks} float32")
+        per_row = 0
+        if mask is not None and n:
+            if mask.dtype != torch.uint8 or not mask.numel() or n % mask.numel():
+                raise ValueError("mask must be uint8, one entry for every row of p")
+            per_row = n // mask.numel()
+        a.n, a.per_row, a.p_dtype, a.g_dtype, a.state_bits = n, per_row, _dtype(p, "p"), _dtype(g, "g"), bits
+        a.d_p, a.d_g, a.d_m, a.d_v = p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr()
+        if bits == 8:
+            a.d_m_scale, a.d_v_scale = t["m_scale"].data_ptr(), t["v_scale"].data_ptr()
+        a.d_mask = mask.data_ptr() if per_row else None
+    return AdamwTensors(arr, [dict(t) for t in tensors])
+
+
+def fp_adamw_step(table, lr, step=1, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=1.0, d_lr=None, d_grad_scale=None,
+                  d_step=None, stream=None):
+    """One AdamW step (number `step`, from 1) over all tensors of a table.  d_lr, d_grad_scale (float32) and d_step (int64): CUDA tensors of
+    one element that are read when the kernel runs, in place of the numbers - for a captured step."""
+    import torch
+    for t, dt, k in ((d_lr, torch.float32, "d_lr"), (d_grad_scale, torch.float32, "d_grad_scale"), (d_step, torch.int64, "d_step")):
+        if t is not None and (t.dtype != dt or t.numel() != 1 or not t.is_cuda):
+            raise ValueError(f"{k}: a CUDA tensor of one {dt} is wanted")
+    h = fp_adamw_hyper(lr, beta1, beta2, eps, weight_decay, grad_scale, step, *(None if t is None else t.data_ptr() for t in (d_lr, d_grad_scale, d_step)))
+    _check(lib().fp_adamw_step(ctypes.addressof(table.array), len(table.array), ctypes.addressof(h),
+                               stream.cuda_stream if stream is not None else None))

@@ -1,0 +1,729 @@
+// Fully connected layers and their gradients (fp_linear_forward, fp_linear_backward).
+//
+// All three products are D(i, j) = sum_k A(i, k) B(j, k) on the tensor cores, which take either operand with k or with i (j)
+// contiguous in memory, so that nothing is transposed beforehand:
+//     y  = x w'    A = x  (rows m, k contiguous)     B = w  (rows n, k contiguous)
+//     dx = dz w    A = dz (rows m, n contiguous)     B = w  read with its rows as the sum's index, its columns contiguous
+//     dw = dz' x   A = dz and B = x, both with the sum's index m as rows
+// Operands come by tensor-map copies (zeros outside the matrix, so ragged sizes need no other code); those need 16-byte
+// aligned rows, and an operand that has none is copied into scratch first.
+#include "train_common.cuh"
+#include "tc_common.cuh"
+
+#include <cuda.h>
+#include <math.h>
+#include <string.h>
+
+#include <algorithm>
+#include <atomic>
+#include <mutex>
+
+namespace fp {
+namespace {
+
+using namespace tc;
+using namespace train;
+
+constexpr int kBlockK = 64;                              // elements of the sum a stage: 128 bytes, a swizzled row
+constexpr int64_t kMaxSize = 1ll << 30;
+constexpr int kMaxSmem = 232448;                         // shared memory a block may have
+
+__device__ int g_linear_status;                          // raised by a bounded wait that ran out
+
+// What is done with a finished sum.  Outputs are rows of n neighbours; the accumulator has n along j, or with `swap` along i.
+struct Epilogue {
+    void* y;
+    void* pre;
+    const void* res;
+    const void* bias;                                    // by n
+    long long ld_y, ld_pre, ld_res;
+    int y_type, pre_type, res_type, bias_type, act, res_first;
+    int vec;                                             // 1: four neighbours of every buffer lie aligned
+};
+struct Problem {
+    CUtensorMap a, b;                                    // boxes of 64 k x rows, or 64 rows x 64 k (…_mn)
+    int I, J, kblocks;
+    int tiles_i, tiles_j, tile0;                         // this problem's tiles are tile0 ..
+    int a_mn, b_mn, swap;
+    Epilogue e;
+};
+struct TileParams {
+    Problem prob[2];
+    int n_prob, splits, stages;
+    uint32_t bf16;
+    int* status;
+};
+
+// Up to four neighbours (row, n .. n + count - 1) of the output from their sums.
+__device__ __forceinline__ void finish4(const Epilogue& e, long long row, int n, int count, float (&v)[4]) {
+    float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const bool whole = e.vec && count == 4;
+    if (e.res) {
+        const long long at = row * e.ld_res + n;
+        if (whole) load4(e.res, at, e.res_type, r);
+        else
+            for (int i = 0; i < 4; ++i) if (i < count) r[i] = load1(e.res, at + i, e.res_type);
+    }
+    if (e.bias)
+        for (int i = 0; i < 4; ++i) if (i < count) v[i] += load1(e.bias, n + i, e.bias_type);
+    if (e.res && e.res_first)
+        for (int i = 0; i < 4; ++i) v[i] += r[i];
+    if (e.pre) {
+        const long long at = row * e.ld_pre + n;
+        if (whole) store4(e.pre, at, e.pre_type, v);
+        else
+            for (int i = 0; i < 4; ++i) if (i < count) store1(e.pre, at + i, e.pre_type, v[i]);
+    }
+    if (e.act != FP_ACT_NONE)
+        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], e.act);
+    if (e.res && !e.res_first)
+        for (int i = 0; i < 4; ++i) v[i] += r[i];
+    const long long at = row * e.ld_y + n;
+    if (whole) store4(e.y, at, e.y_type, v);
+    else
+        for (int i = 0; i < 4; ++i) if (i < count) store1(e.y, at + i, e.y_type, v[i]);
+}
+
+// ---- one 128 x BN tile a cluster ------------------------------------------------------------------------------------
+// `splits` CTAs share a tile's sum, a range of K blocks each; their partial sums meet in shared memory, where every
+// CTA finishes its part of the tile (the terms in the CTAs' order: one order of sums for a size).  With few rows (M <= 128)
+// the weights take the 128 rows of the tensor core's tile and the activations its BN columns: a single token then costs 16 columns instead
+// of 128 rows, and the weights' bytes are all that counts.
+
+constexpr int kTileThreads = 256;
+struct TileCtrl {
+    uint64_t full[16], empty[16], done;
+    uint32_t tmem;
+    int abort_flag;
+};
+
+__device__ __forceinline__ void lds16_cluster(uint32_t addr, float (&v)[4]) {
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr) : "memory");
+}
+
+template <int BN>
+__global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_constant__ TileParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ TileCtrl ctrl;
+    constexpr uint32_t kStage = 128 * 128 + BN * 128;
+    constexpr int kCols = BN < 32 ? 32 : BN;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = p.splits > 1 ? cluster_rank() : 0u;
+    const int tile_all = (int)(blockIdx.x / (unsigned)p.splits);
+    const Problem& q = p.prob[p.n_prob > 1 && tile_all >= p.prob[1].tile0 ? 1 : 0];
+    const int tile = tile_all - q.tile0;
+    // Eight row tiles at a time over all column tiles: what runs at once reads a square of the product's operands.
+    const int group = tile / (8 * q.tiles_j), in_group = tile - group * 8 * q.tiles_j;
+    const int rows_here = min(8, q.tiles_i - group * 8);
+    const int i0 = (group * 8 + in_group % rows_here) * 128, j0 = (in_group / rows_here) * BN;
+    const int kb0 = (int)((long long)q.kblocks * rank / p.splits), kb1 = (int)((long long)q.kblocks * (rank + 1) / p.splits);
+    volatile int* abort_flag = &ctrl.abort_flag;
+    const uint32_t full0 = smem_u32(ctrl.full), empty0 = smem_u32(ctrl.empty), done = smem_u32(&ctrl.done);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            prefetch_map(&q.a);
+            prefetch_map(&q.b);
+            for (int s = 0; s < p.stages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+            mbar_init(done, 1);
+            ctrl.abort_flag = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+    } else if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl.tmem)), "r"((uint32_t)kCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ctrl.tmem;
+    bool ok = true;
+    if (warp == 0) {
+        int stage = 0;
+        uint32_t phase = 0;
+        for (int kb = kb0; kb < kb1; ++kb) {
+            if (kb - kb0 >= p.stages) ok = __all_sync(0xffffffffu, mbar_wait(empty0 + 8 * stage, phase ^ 1u, abort_flag));
+            if (!ok) break;
+            if (elect_one()) {
+                const uint32_t bar = full0 + 8 * stage, a = base + (uint32_t)stage * kStage, b = a + 128 * 128;
+                mbar_expect_tx(bar, kStage);
+                const int k = kb * kBlockK;
+                if (q.a_mn) {
+                    tma_load_2d(a, &q.a, i0, k, bar);
+                    tma_load_2d(a + 8192, &q.a, i0 + 64, k, bar);
+                } else {
+                    tma_load_2d(a, &q.a, k, i0, bar);
+                }
+                if (q.b_mn) {
+                    tma_load_2d(b, &q.b, j0, k, bar);
+                    if (BN > 64) tma_load_2d(b + 8192, &q.b, j0 + 64, k, bar);
+                } else {
+                    tma_load_2d(b, &q.b, k, j0, bar);
+                }
+            }
+            __syncwarp();
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+    } else if (warp == 1) {
+        const uint32_t idesc = f16_idesc((int)p.bf16, q.a_mn, q.b_mn, 128, BN);
+        const uint32_t a_step = q.a_mn ? 128u : 2u, b_step = q.b_mn ? 128u : 2u;
+        int stage = 0;
+        uint32_t phase = 0;
+        for (int kb = kb0; kb < kb1; ++kb) {
+            ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8 * stage, phase, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t a = base + (uint32_t)stage * kStage;
+            const uint32_t al = sw128_lo(a, 8192), bl = sw128_lo(a + 128 * 128, 8192), leader = elect_one();
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                umma_sw128_if(leader, tmem, al + (uint32_t)s * a_step, bl + (uint32_t)s * b_step, idesc, kb > kb0 || s ? 1u : 0u);
+            if (leader) {
+                umma_commit(empty0 + 8 * stage);
+                if (kb == kb1 - 1) umma_commit(done);
+            }
+            __syncwarp();
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+        }
+    }
+    if (!ok && lane == 0) { atomicExch(&ctrl.abort_flag, 1); atomicExch(p.status, 1); }
+    if (kb1 > kb0 && ok) {
+        ok = __all_sync(0xffffffffu, mbar_wait(done, 0, abort_flag));
+        if (!ok && lane == 0) { atomicExch(&ctrl.abort_flag, 1); atomicExch(p.status, 1); }
+    }
+    tc_fence_after();
+    if (*abort_flag)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);         // copies in flight land before the memory is used again
+    __syncthreads();                                             // every stage has been read: its memory takes the sums now
+
+    // Sums in shared memory with n along a row: [i][j], or with swap [j][i].  Pitches of 4 (mod 32) words keep 16-byte
+    // accesses of neighbouring lanes in different banks.
+    const int pitch = q.swap ? 132 : BN + 4;
+    {
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        constexpr int kChunks = BN / 8;
+#pragma unroll 1
+        for (int c = warp >> 2; c < kChunks; c += 2) {
+            uint32_t v[8];
+            tmem_ld8(taddr + (uint32_t)(8 * c), v);
+            tmem_ld_wait();
+            if (kb1 <= kb0)
+                for (int i = 0; i < 8; ++i) v[i] = 0;
+            if (q.swap) {
+                const uint32_t to = base + (uint32_t)(8 * c * pitch + row) * 4u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + (uint32_t)(i * pitch) * 4u), "r"(v[i]) : "memory");
+            } else {
+                const uint32_t to = base + (uint32_t)(row * pitch + 8 * c) * 4u;
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+            }
+        }
+    }
+    tc_fence_before();
+    if (p.splits > 1) cluster_sync_all();
+    else __syncthreads();
+    {
+        const int r0 = q.swap ? j0 : i0, n0 = q.swap ? i0 : j0;
+        const int rows = min(q.swap ? BN : 128, (q.swap ? q.J : q.I) - r0), N = q.swap ? q.I : q.J;
+        const int per_row = (q.swap ? 128 : BN) / 4, total = rows * per_row;
+        const int from = (int)((long long)total * rank / p.splits), to = (int)((long long)total * (rank + 1) / p.splits);
+        for (int x = from + (int)threadIdx.x; x < to; x += kTileThreads) {
+            const int r = x / per_row, c = (x - r * per_row) * 4;
+            const int count = min(4, N - (n0 + c));
+            if (count <= 0) continue;
+            const uint32_t at = base + (uint32_t)(r * pitch + c) * 4u;
+            float v[4];
+            if (p.splits == 1) {
+                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(at) : "memory");
+            } else {
+                lds16_cluster(cluster_addr(at, 0), v);
+                for (int s = 1; s < p.splits; ++s) {
+                    float u[4];
+                    lds16_cluster(cluster_addr(at, (uint32_t)s), u);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] += u[i];
+                }
+            }
+            finish4(q.e, r0 + r, n0 + c, count, v);
+        }
+    }
+    if (p.splits > 1) cluster_sync_all();                        // no CTA leaves while another may still read its sums
+    else __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kCols) : "memory");
+    }
+}
+
+// ---- operands that tensor-map copies cannot read --------------------------------------------------------------------
+
+struct CopyJob {
+    const uint16_t* src;
+    uint16_t* dst;
+    long long ld_src, ld_dst, rows;
+    int cols, chunks;                                    // chunks of 512 elements a row
+    long long warp0;
+};
+struct CopyParams { CopyJob job[2]; long long warps; };
+
+// Rows of 16-bit elements of any alignment into rows that start at 16-byte boundaries.  A warp moves 512 elements, 64 bytes an
+// instruction: whatever the alignment the lines are used whole.
+__global__ void __launch_bounds__(256) copy_rows_kernel(const CopyParams p) {
+    const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (w >= p.warps) return;
+    const CopyJob& j = p.job[w >= p.job[1].warp0 ? 1 : 0];
+    const long long u = w - j.warp0, row = u / j.chunks;
+    const int c0 = (int)(u - row * j.chunks) * 512 + (threadIdx.x & 31);
+    const uint16_t* s = j.src + row * j.ld_src;
+    uint16_t* d = j.dst + row * j.ld_dst;
+    uint16_t v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = c0 + 32 * i < j.cols ? s[c0 + 32 * i] : (uint16_t)0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (c0 + 32 * i < j.cols) d[c0 + 32 * i] = v[i];
+}
+
+// ---- dz and the bias's gradient -------------------------------------------------------------------------------------
+// dz = dy * act'(pre), rounded into up to two places, and its column sums.  A cluster of CTAs has 128 columns; each CTA takes a
+// range of rows, its warps every eighth row of it.  Column sums: a thread's rows, then the eight warps, then the CTAs, each in
+// order.
+
+struct DzParams {
+    const uint16_t* dy;
+    const uint16_t* pre;
+    uint16_t* out[2];
+    void* db;
+    long long ld_dy, ld_pre, ld_out[2], M;
+    int N, act, dtype, db_type, accumulate, splits;
+};
+
+template <bool VEC>
+__global__ void __launch_bounds__(256) linear_dz_kernel(const DzParams p) {
+    __shared__ float part[8][128];
+    __shared__ __align__(16) float sums[128];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int split = (int)(blockIdx.x % (unsigned)p.splits);
+    const int n0 = (int)(blockIdx.x / (unsigned)p.splits) * 128;
+    const long long m0 = p.M * split / p.splits, m1 = p.M * (split + 1) / p.splits;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    // columns of a thread: four neighbours, or (rows that are not aligned) every 32nd
+    int col[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) col[i] = n0 + (VEC ? 4 * lane + i : lane + 32 * i);
+    auto load = [&](const uint16_t* base, long long row, float (&v)[4]) {
+        if (VEC) { if (col[0] < p.N) load4(base, row + col[0], p.dtype, v); }
+        else
+            for (int i = 0; i < 4; ++i) if (col[i] < p.N) v[i] = to_f32(base[row + col[i]], p.dtype);
+    };
+    constexpr int kRows = 4;                             // rows a thread has in flight
+#pragma unroll 1
+    for (long long m = m0 + warp; m < m1; m += 8 * kRows) {
+        float g[kRows][4], z[kRows][4];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) g[r][i] = z[r][i] = 0.0f;
+            if (m + 8 * r < m1) {
+                load(p.dy, (m + 8 * r) * p.ld_dy, g[r]);
+                if (p.act != FP_ACT_NONE) load(p.pre, (m + 8 * r) * p.ld_pre, z[r]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (m + 8 * r >= m1) break;
+            if (p.act != FP_ACT_NONE)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) g[r][i] *= act_grad(z[r][i], p.act);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] += g[r][i];
+#pragma unroll
+            for (int o = 0; o < 2; ++o)
+                if (p.out[o]) {
+                    const long long at = (m + 8 * r) * p.ld_out[o];
+                    if (VEC) { if (col[0] < p.N) store4(p.out[o], at + col[0], p.dtype, g[r]); }
+                    else
+                        for (int i = 0; i < 4; ++i) if (col[i] < p.N) p.out[o][at + col[i]] = to_16(g[r][i], p.dtype);
+                }
+        }
+    }
+    if (!p.db) return;                                   // (the same for all CTAs of a cluster)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) part[warp][col[i] - n0] = s[i];
+    __syncthreads();
+    float v = 0.0f;
+    if (threadIdx.x < 128) {
+        for (int w = 0; w < 8; ++w) v += part[w][threadIdx.x];
+        sums[threadIdx.x] = v;
+    }
+    if (p.splits > 1) cluster_sync_all();
+    if (split == 0 && threadIdx.x < 128) {
+        for (int c = 1; c < p.splits; ++c) {
+            float u;
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u) : "r"(cluster_addr(smem_u32(&sums[threadIdx.x]), (uint32_t)c)) : "memory");
+            v += u;
+        }
+        const int n = n0 + (int)threadIdx.x;
+        if (n < p.N) store1(p.db, n, p.db_type, p.accumulate ? load1(p.db, n, p.db_type) + v : v);
+    }
+    if (p.splits > 1) cluster_sync_all();
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// A matrix of `rows` rows of `cols` contiguous 16-bit elements; boxes of 64 x box_rows.
+bool make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows, int dtype) {
+    static std::atomic<void*> known;
+    const EncodeTiled encode = (EncodeTiled)driver_function("cuTensorMapEncodeTiled", &known);
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? ld : (cols + 7) / 8 * 8) * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, one[2] = {1, 1};
+    return encode(map, dtype == FP_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(base), dims,
+                  strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool readable(const void* p, int64_t rows, int64_t ld) { return ((uintptr_t)p & 15) == 0 && (rows <= 1 || (ld & 7) == 0); }
+bool aligned4(const void* p, int64_t ld, int dtype, int64_t rows) {
+    return ((uintptr_t)p & (uintptr_t)(4 * elem_bytes(dtype) - 1)) == 0 && (rows <= 1 || (ld & 3) == 0);
+}
+size_t packed_bytes(int64_t rows, int64_t cols) { return ((size_t)rows * (size_t)((cols + 7) / 8 * 8) * 2 + 255) / 256 * 256; }
+
+int* status_word(int dev) {
+    static std::atomic<int*> known[64];
+    if (dev < 0 || dev >= 64) return nullptr;
+    int* p = known[dev].load(std::memory_order_acquire);
+    if (!p) {
+        if (cudaGetSymbolAddress((void**)&p, g_linear_status) != cudaSuccess) { cudaGetLastError(); return nullptr; }
+        known[dev].store(p, std::memory_order_release);
+    }
+    return p;
+}
+
+template <int BN>
+cudaError_t launch_tiles_bn(const TileParams& p, int tiles, int smem, cudaStream_t st) {
+    // (set at every call, as it is kept for each device by itself and costs nothing beside the launch)
+    cudaError_t e = cudaFuncSetAttribute(linear_tile_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem - (int)sizeof(TileCtrl) - 64);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3((unsigned)(tiles * p.splits));
+    cfg.blockDim = dim3(kTileThreads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)p.splits;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, linear_tile_kernel<BN>, p);
+}
+
+struct Operand { const void* p; int64_t rows, cols, ld; int mn; };   // mn: rows are the sum's index
+struct Product { Operand a, b; int64_t I, J, Kc; int swap; Epilogue e; };
+
+// All products of a call in one launch.
+fp_status run_products(const Product* prod, int n, int dtype, int* status, cudaStream_t st) {
+    TileParams p;
+    memset(&p, 0, sizeof(p));
+    int64_t tiles = 0, kblocks = 1 << 30;
+    int bn = 128;
+    if (n == 1 && prod[0].swap) bn = prod[0].J <= 16 ? 16 : prod[0].J <= 32 ? 32 : prod[0].J <= 64 ? 64 : 128;
+    for (int i = 0; i < n; ++i) {
+        const Product& r = prod[i];
+        Problem& q = p.prob[i];
+        q.I = (int)r.I; q.J = (int)r.J; q.kblocks = (int)((r.Kc + kBlockK - 1) / kBlockK);
+        q.tiles_i = (int)((r.I + 127) / 128); q.tiles_j = (int)((r.J + bn - 1) / bn);
+        if (tiles + (int64_t)q.tiles_i * q.tiles_j > (1 << 27)) return err(FP_ERR_BOUNDS, "fp_linear: more tiles than a launch takes");
+        q.tile0 = (int)tiles;
+        tiles += (int64_t)q.tiles_i * q.tiles_j;
+        kblocks = std::min<int64_t>(kblocks, q.kblocks);
+        q.a_mn = r.a.mn; q.b_mn = r.b.mn; q.swap = r.swap; q.e = r.e;
+        if (!make_map(&q.a, r.a.p, r.a.rows, r.a.cols, r.a.ld, r.a.mn ? 64 : 128, dtype) ||
+            !make_map(&q.b, r.b.p, r.b.rows, r.b.cols, r.b.ld, r.b.mn ? 64 : bn, dtype))
+            return err(FP_ERR_CUDA, "fp_linear: an operand's tensor map was refused");
+    }
+    p.n_prob = n; p.status = status; p.bf16 = dtype == FP_DTYPE_BF16;
+    const int sms = sm_count();
+    p.splits = 1;
+    while (p.splits < 8 && tiles * p.splits * 2 <= sms && kblocks >= p.splits * 4) p.splits *= 2;
+    const int stage = 128 * 128 + bn * 128, per_cta = (int)((kblocks + p.splits - 1) / p.splits);
+    int64_t most = 0;
+    for (int i = 0; i < n; ++i) most = std::max<int64_t>(most, (p.prob[i].kblocks + p.splits - 1) / p.splits);
+    (void)per_cta;
+    const int room = tiles * p.splits > sms ? kMaxSmem / 2 - 3072 : kMaxSmem - 3072;
+    p.stages = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(room / stage, 16), most));
+    const int sums = prod[0].swap ? bn * 132 * 4 : 128 * (bn + 4) * 4;
+    const int smem = std::max(p.stages * stage, sums) + 1024;
+    cudaError_t e = bn == 16 ? launch_tiles_bn<16>(p, (int)tiles, smem, st) : bn == 32 ? launch_tiles_bn<32>(p, (int)tiles, smem, st)
+                  : bn == 64 ? launch_tiles_bn<64>(p, (int)tiles, smem, st) : launch_tiles_bn<128>(p, (int)tiles, smem, st);
+    if (e != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, cudaGetErrorString(e)); }
+    return FP_OK;
+}
+
+fp_status copy_rows(const CopyJob* jobs, int n, cudaStream_t st) {
+    CopyParams p;
+    memset(&p, 0, sizeof(p));
+    p.job[1].warp0 = 1ll << 62;
+    for (int i = 0; i < n; ++i) {
+        p.job[i] = jobs[i];
+        p.job[i].chunks = (jobs[i].cols + 511) / 512;
+        p.job[i].warp0 = p.warps;
+        p.warps += p.job[i].rows * p.job[i].chunks;
+    }
+    if ((p.warps + 7) / 8 > 0x7fffffffll) return err(FP_ERR_BOUNDS, "fp_linear: operand too large");
+    copy_rows_kernel<<<(unsigned)((p.warps + 7) / 8), 256, 0, st>>>(p);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? FP_OK : err(FP_ERR_CUDA, cudaGetErrorString(e));
+}
+
+// Takes an operand into scratch where it cannot be read in place.
+const void* place(const void* src, int64_t rows, int64_t cols, int64_t* ld, char** work, CopyJob* jobs, int* n_jobs) {
+    if (readable(src, rows, *ld)) return src;
+    CopyJob& j = jobs[(*n_jobs)++];
+    memset(&j, 0, sizeof(j));
+    j.src = static_cast<const uint16_t*>(src);
+    j.dst = reinterpret_cast<uint16_t*>(*work);
+    j.rows = rows; j.cols = (int)cols; j.ld_src = *ld; j.ld_dst = (cols + 7) / 8 * 8;
+    *ld = j.ld_dst;
+    *work += packed_bytes(rows, cols);
+    return j.dst;
+}
+
+bool sizes_ok(int64_t M, int64_t N, int64_t K) { return M >= 0 && N >= 1 && K >= 1; }
+bool in_bounds(int64_t M, int64_t N, int64_t K) { return M <= kMaxSize && N <= kMaxSize && K <= kMaxSize; }
+// Rows of `cols` elements: the stride must reach over a row and stay within what a tensor map can hold.
+bool ld_ok(int64_t ld, int64_t cols, int64_t rows) { return rows <= 1 ? true : ld >= cols && ld <= (1ll << 38); }
+
+fp_status check(const fp_linear_args* a) {
+    if (!a) return err(FP_ERR_ARG, "fp_linear_forward: NULL argument");
+    if (!sizes_ok(a->M, a->N, a->K)) return err(FP_ERR_ARG, "fp_linear_forward: bad sizes (M >= 0, N and K >= 1)");
+    if (!in_bounds(a->M, a->N, a->K)) return err(FP_ERR_BOUNDS, "fp_linear_forward: a size beyond 2^30");
+    if (!is_half(a->dtype)) return err(FP_ERR_UNSUPPORTED, "fp_linear_forward: dtype must be FP_DTYPE_BF16 or FP_DTYPE_F16");
+    if ((a->y_dtype != a->dtype && a->y_dtype != FP_DTYPE_F32) || (a->d_bias && a->bias_dtype != a->dtype && a->bias_dtype != FP_DTYPE_F32))
+        return err(FP_ERR_UNSUPPORTED, "fp_linear_forward: y and bias have dtype, or FP_DTYPE_F32");
+    if (a->act < FP_ACT_NONE || a->act > FP_ACT_SILU || (a->res_first != 0 && a->res_first != 1) || a->reserved)
+        return err(FP_ERR_ARG, "fp_linear_forward: bad activation, res_first or reserved");
+    if (a->M == 0) return FP_OK;
+    if (!a->d_x || !a->d_w || !a->d_y) return err(FP_ERR_ARG, "fp_linear_forward: NULL x, w or y");
+    if (!ld_ok(a->ld_x, a->K, a->M) || !ld_ok(a->ld_w, a->K, a->N) || !ld_ok(a->ld_y, a->N, a->M) || (a->d_res && !ld_ok(a->ld_res, a->N, a->M)) ||
+        (a->d_pre && !ld_ok(a->ld_pre, a->N, a->M)))
+        return err(FP_ERR_ARG, "fp_linear_forward: a row stride is shorter than its row");
+    const uintptr_t odd = (uintptr_t)a->d_x | (uintptr_t)a->d_w | (uintptr_t)a->d_res | (uintptr_t)a->d_pre;
+    if ((odd & 1) || ((uintptr_t)a->d_y & (uintptr_t)(elem_bytes(a->y_dtype) - 1)) || ((uintptr_t)a->d_bias & (uintptr_t)(elem_bytes(a->bias_dtype) - 1)))
+        return err(FP_ERR_ARG, "fp_linear_forward: a buffer is not aligned to its elements");
+    return FP_OK;
+}
+
+size_t forward_work(const fp_linear_args* a) {
+    if (a->M == 0) return 0;
+    return (readable(a->d_x, a->M, a->ld_x) ? 0 : packed_bytes(a->M, a->K)) + (readable(a->d_w, a->N, a->ld_w) ? 0 : packed_bytes(a->N, a->K));
+}
+
+fp_status check(const fp_linear_grad_args* a) {
+    if (!a) return err(FP_ERR_ARG, "fp_linear_backward: NULL argument");
+    if (!sizes_ok(a->M, a->N, a->K)) return err(FP_ERR_ARG, "fp_linear_backward: bad sizes (M >= 0, N and K >= 1)");
+    if (!in_bounds(a->M, a->N, a->K)) return err(FP_ERR_BOUNDS, "fp_linear_backward: a size beyond 2^30");
+    if (!is_half(a->dtype) || (a->dw_dtype != a->dtype && a->dw_dtype != FP_DTYPE_F32))
+        return err(FP_ERR_UNSUPPORTED, "fp_linear_backward: dtype must be FP_DTYPE_BF16 or FP_DTYPE_F16, dw_dtype the same or FP_DTYPE_F32");
+    if (a->act < FP_ACT_NONE || a->act > FP_ACT_SILU || (a->accumulate != 0 && a->accumulate != 1))
+        return err(FP_ERR_ARG, "fp_linear_backward: bad activation or accumulate");
+    if (!a->d_dw && !a->d_db && !(a->M == 0 || a->d_dx || a->d_dz)) return err(FP_ERR_ARG, "fp_linear_backward: no output is asked for");
+    if (a->d_dw && !ld_ok(a->ld_dw, a->K, a->N)) return err(FP_ERR_ARG, "fp_linear_backward: a row stride is shorter than its row");
+    const uintptr_t outs = (uintptr_t)a->d_dw | (uintptr_t)a->d_db;
+    if (outs & (uintptr_t)(elem_bytes(a->dw_dtype) - 1)) return err(FP_ERR_ARG, "fp_linear_backward: a buffer is not aligned to its elements");
+    if (a->M == 0) return FP_OK;
+    if (!a->d_dy || (a->act != FP_ACT_NONE && !a->d_pre) || (a->d_dw && !a->d_x) || (a->d_dx && !a->d_w))
+        return err(FP_ERR_ARG, "fp_linear_backward: NULL dy, pre (with an activation), x (for dw) or w (for dx)");
+    if (!ld_ok(a->ld_dy, a->N, a->M) || (a->act != FP_ACT_NONE && !ld_ok(a->ld_pre, a->N, a->M)) || (a->d_dw && !ld_ok(a->ld_x, a->K, a->M)) ||
+        (a->d_dx && (!ld_ok(a->ld_w, a->K, a->N) || !ld_ok(a->ld_dx, a->K, a->M))) || (a->d_dz && !ld_ok(a->ld_dz, a->N, a->M)))
+        return err(FP_ERR_ARG, "fp_linear_backward: a row stride is shorter than its row");
+    if (a->d_dz == a->d_dy && a->M > 1 && a->ld_dz != a->ld_dy) return err(FP_ERR_ARG, "fp_linear_backward: dz in dy's place needs dy's row stride");
+    const uintptr_t odd = (uintptr_t)a->d_dy | (uintptr_t)a->d_pre | (uintptr_t)a->d_x | (uintptr_t)a->d_w | (uintptr_t)a->d_dx | (uintptr_t)a->d_dz;
+    if (odd & 1) return err(FP_ERR_ARG, "fp_linear_backward: a buffer is not aligned to its elements");
+    return FP_OK;
+}
+
+// Whether the products need a dz of their own in scratch: where there is no tensor that they can read in place.
+bool dz_in_work(const fp_linear_grad_args* a) {
+    if (!a->d_dx && !a->d_dw) return false;
+    if (a->d_dz && readable(a->d_dz, a->M, a->ld_dz)) return false;
+    return a->act != FP_ACT_NONE || !readable(a->d_dy, a->M, a->ld_dy);
+}
+size_t backward_work(const fp_linear_grad_args* a) {
+    if (a->M == 0) return 0;
+    return (dz_in_work(a) ? packed_bytes(a->M, a->N) : 0) + (a->d_dw && !readable(a->d_x, a->M, a->ld_x) ? packed_bytes(a->M, a->K) : 0) +
+           (a->d_dx && !readable(a->d_w, a->N, a->ld_w) ? packed_bytes(a->N, a->K) : 0);
+}
+fp_status check_work(const void* work, size_t have, size_t need, Buffers& buf) {
+    if (need == 0) return FP_OK;
+    if (!work || have < need) return err(FP_ERR_BOUNDS, "fp_linear: the scratch is smaller than the workspace call says");
+    if ((uintptr_t)work & 255) return err(FP_ERR_ARG, "fp_linear: the scratch is not aligned to 256 bytes");
+    return buf.here(work) ? FP_OK : err(FP_ERR_ARG, "fp_linear: the scratch is not memory of the current device");
+}
+
+}  // namespace
+}  // namespace fp
+
+using namespace fp;
+using namespace fp::train;
+
+extern "C" fp_status fp_linear_workspace(const fp_linear_args* a, size_t* bytes) {
+    if (!bytes) return err(FP_ERR_ARG, "fp_linear_workspace: NULL argument");
+    const fp_status s = check(a);
+    if (s == FP_OK) *bytes = forward_work(a);
+    return s;
+}
+
+extern "C" fp_status fp_linear_backward_workspace(const fp_linear_grad_args* a, size_t* bytes) {
+    if (!bytes) return err(FP_ERR_ARG, "fp_linear_backward_workspace: NULL argument");
+    const fp_status s = check(a);
+    if (s == FP_OK) *bytes = backward_work(a);
+    return s;
+}
+
+extern "C" fp_status fp_linear_forward(const fp_linear_args* a, void* work, size_t work_bytes, void* stream) {
+    fp_status s = check(a);
+    if (s != FP_OK || a->M == 0) return s;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, "fp_linear_forward: no current device"); }
+    Buffers buf(dev);
+    if (!buf.here(a->d_x) || !buf.here(a->d_w) || !buf.here(a->d_y) || !buf.here_or_null(a->d_bias) ||
+        !buf.here_or_null(a->d_res) || !buf.here_or_null(a->d_pre))
+        return err(FP_ERR_ARG, "fp_linear_forward: a buffer is not memory of the current device");
+    if ((s = check_work(work, work_bytes, forward_work(a), buf)) != FP_OK) return s;
+    int* status = status_word(dev);
+    if (!status) return err(FP_ERR_CUDA, "fp_linear_forward: no status word on this device");
+    const cudaStream_t st = (cudaStream_t)stream;
+    char* w = static_cast<char*>(work);
+    CopyJob jobs[2];
+    int n_jobs = 0;
+    int64_t ld_x = a->ld_x, ld_w = a->ld_w;
+    const void* x = place(a->d_x, a->M, a->K, &ld_x, &w, jobs, &n_jobs);
+    const void* wt = place(a->d_w, a->N, a->K, &ld_w, &w, jobs, &n_jobs);
+    if (n_jobs && (s = copy_rows(jobs, n_jobs, st)) != FP_OK) return s;
+    Product p;
+    memset(&p, 0, sizeof(p));
+    const Operand ox = {x, a->M, a->K, ld_x, 0}, ow = {wt, a->N, a->K, ld_w, 0};
+    p.swap = a->M <= 128;
+    p.a = p.swap ? ow : ox; p.b = p.swap ? ox : ow;
+    p.I = p.swap ? a->N : a->M; p.J = p.swap ? a->M : a->N; p.Kc = a->K;
+    Epilogue& e = p.e;
+    e.y = a->d_y; e.pre = a->d_pre; e.res = a->d_res; e.bias = a->d_bias;
+    e.ld_y = a->ld_y; e.ld_pre = a->ld_pre; e.ld_res = a->ld_res;
+    e.y_type = a->y_dtype; e.pre_type = e.res_type = a->dtype; e.bias_type = a->bias_dtype; e.act = a->act; e.res_first = a->res_first;
+    e.vec = aligned4(a->d_y, a->ld_y, a->y_dtype, a->M) && (!a->d_pre || aligned4(a->d_pre, a->ld_pre, a->dtype, a->M)) &&
+            (!a->d_res || aligned4(a->d_res, a->ld_res, a->dtype, a->M));
+    return run_products(&p, 1, a->dtype, status, st);
+}
+
+extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work, size_t work_bytes, void* stream) {
+    fp_status s = check(a);
+    if (s != FP_OK) return s;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, "fp_linear_backward: no current device"); }
+    Buffers buf(dev);
+    if (!buf.here_or_null(a->d_dw) || !buf.here_or_null(a->d_db) ||
+        (a->M > 0 && (!buf.here(a->d_dy) || (a->act != FP_ACT_NONE && !buf.here(a->d_pre)) || (a->d_dw && !buf.here(a->d_x)) ||
+                      (a->d_dx && !buf.here(a->d_w)) || !buf.here_or_null(a->d_dx) || !buf.here_or_null(a->d_dz))))
+        return err(FP_ERR_ARG, "fp_linear_backward: a buffer is not memory of the current device");
+    const cudaStream_t st = (cudaStream_t)stream;
+    const int dw_bytes = elem_bytes(a->dw_dtype);
+    if (a->M == 0) {                                     // empty sums
+        cudaError_t e = cudaSuccess;
+        if (!a->accumulate && a->d_dw)
+            e = cudaMemset2DAsync(a->d_dw, (size_t)std::max(a->N > 1 ? a->ld_dw : 0, a->K) * dw_bytes, 0, (size_t)a->K * dw_bytes, (size_t)a->N, st);
+        if (e == cudaSuccess && !a->accumulate && a->d_db) e = cudaMemsetAsync(a->d_db, 0, (size_t)a->N * dw_bytes, st);
+        if (e != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, cudaGetErrorString(e)); }
+        return FP_OK;
+    }
+    if ((s = check_work(work, work_bytes, backward_work(a), buf)) != FP_OK) return s;
+    int* status = status_word(dev);
+    if (!status) return err(FP_ERR_CUDA, "fp_linear_backward: no status word on this device");
+    char* w = static_cast<char*>(work);
+    // dz: where the products read it, and what has to be written for that
+    const void* dz = a->d_dy;
+    int64_t ld_dz = a->ld_dy;
+    DzParams d;
+    memset(&d, 0, sizeof(d));
+    if (a->d_dz) { d.out[0] = static_cast<uint16_t*>(a->d_dz); d.ld_out[0] = a->ld_dz; dz = a->d_dz; ld_dz = a->ld_dz; }
+    if (dz_in_work(a)) {
+        d.out[1] = reinterpret_cast<uint16_t*>(w);
+        d.ld_out[1] = (a->N + 7) / 8 * 8;
+        w += packed_bytes(a->M, a->N);
+        dz = d.out[1]; ld_dz = d.ld_out[1];
+    }
+    if (d.out[0] || d.out[1] || a->d_db) {
+        d.dy = static_cast<const uint16_t*>(a->d_dy); d.pre = static_cast<const uint16_t*>(a->d_pre); d.db = a->d_db;
+        d.ld_dy = a->ld_dy; d.ld_pre = a->ld_pre; d.M = a->M; d.N = (int)a->N; d.act = a->act; d.dtype = a->dtype; d.db_type = a->dw_dtype;
+        d.accumulate = a->accumulate;
+        const int64_t blocks = (a->N + 127) / 128;
+        d.splits = 1;
+        while (d.splits < 8 && a->M > 32 * d.splits && blocks * d.splits < 8 * sm_count()) d.splits *= 2;
+        const bool vec = (a->N & 3) == 0 && aligned4(a->d_dy, a->ld_dy, a->dtype, a->M) &&
+                         (a->act == FP_ACT_NONE || aligned4(a->d_pre, a->ld_pre, a->dtype, a->M)) && (!a->d_dz || aligned4(a->d_dz, a->ld_dz, a->dtype, a->M));
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        cfg.gridDim = dim3((unsigned)(blocks * d.splits));
+        cfg.blockDim = dim3(256);
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)d.splits;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        const cudaError_t e = vec ? cudaLaunchKernelEx(&cfg, linear_dz_kernel<true>, d) : cudaLaunchKernelEx(&cfg, linear_dz_kernel<false>, d);
+        if (e != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, cudaGetErrorString(e)); }
+    }
+    if (!a->d_dx && !a->d_dw) return FP_OK;
+    CopyJob jobs[2];
+    int n_jobs = 0, n = 0;
+    int64_t ld_x = a->ld_x, ld_w = a->ld_w;
+    const void* x = a->d_dw ? place(a->d_x, a->M, a->K, &ld_x, &w, jobs, &n_jobs) : nullptr;
+    const void* wt = a->d_dx ? place(a->d_w, a->N, a->K, &ld_w, &w, jobs, &n_jobs) : nullptr;
+    if (n_jobs && (s = copy_rows(jobs, n_jobs, st)) != FP_OK) return s;
+    Product p[2];
+    memset(p, 0, sizeof(p));
+    if (a->d_dx) {
+        Product& r = p[n++];
+        const Operand odz = {dz, a->M, a->N, ld_dz, 0}, ow = {wt, a->N, a->K, ld_w, 1};
+        r.swap = a->M <= 128 && !a->d_dw;
+        r.a = r.swap ? ow : odz; r.b = r.swap ? odz : ow;
+        r.I = r.swap ? a->K : a->M; r.J = r.swap ? a->M : a->K; r.Kc = a->N;
+        r.e.y = a->d_dx; r.e.ld_y = a->ld_dx; r.e.y_type = a->dtype;
+        r.e.vec = aligned4(a->d_dx, a->ld_dx, a->dtype, a->M);
+    }
+    if (a->d_dw) {
+        Product& r = p[n++];
+        r.a = {dz, a->M, a->N, ld_dz, 1}; r.b = {x, a->M, a->K, ld_x, 1};
+        r.I = a->N; r.J = a->K; r.Kc = a->M;
+        r.e.y = a->d_dw; r.e.ld_y = a->ld_dw; r.e.y_type = a->dw_dtype;
+        if (a->accumulate) { r.e.res = a->d_dw; r.e.ld_res = a->ld_dw; r.e.res_type = a->dw_dtype; }
+        r.e.vec = aligned4(a->d_dw, a->ld_dw, a->dw_dtype, a->N);
+    }
+    return run_products(p, n, a->dtype, status, st);
+}
+
+extern "C" fp_status fp_linear_status(int32_t* out) {
+    if (!out) return err(FP_ERR_ARG, "fp_linear_status: NULL argument");
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, "fp_linear_status: no current device"); }
+    int* word = status_word(dev);
+    int v = 0;
+    if (!word || cudaDeviceSynchronize() != cudaSuccess || cudaMemcpy(&v, word, sizeof(v), cudaMemcpyDeviceToHost) != cudaSuccess ||
+        (v && cudaMemset(word, 0, sizeof(v)) != cudaSuccess)) {
+        cudaGetLastError();
+        return err(FP_ERR_CUDA, "fp_linear_status: the status word cannot be read");
+    }
+    *out = v ? FP_ERR_TIMEOUT : FP_OK;
+    return FP_OK;
+}

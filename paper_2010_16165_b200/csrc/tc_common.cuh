@@ -147,6 +147,78 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
 }
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
+// ---- tensor-map copies and operands of any major order (128-byte swizzle) ---------------------------------------------
+
+// A box of a 2-D tensor map -> shared memory; x is the coordinate along the contiguous dimension (a multiple of 16 bytes).
+// Rows of 128 bytes, 16-byte units exchanged within each 8 rows (swizzle 128B); dst 1024-byte aligned; zeros outside.
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// The same for a CTA pair: `bar` is a shared::cluster address and may be the other CTA's.
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const void* map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void prefetch_map(const void* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+
+// Operand descriptor words, 128-byte swizzle.  K-major: rows of 64 K elements, 8-row groups 1024 bytes apart; 16 K elements
+// further is 32 bytes further.  MN-major: rows of 64 M (or N) elements, one per K; 8-K groups 1024 bytes apart, the next 64
+// M elements `mn_bytes` further; 16 K elements further is 2048 bytes further.
+// (Within a cluster a shared address carries the CTA's number above its 18 bits, which would run into the field of mn_bytes.)
+__device__ __forceinline__ uint32_t sw128_lo(uint32_t addr, uint32_t mn_bytes) { return ((addr & 0x3ffffu) >> 4) | ((mn_bytes >> 4) << 16); }
+constexpr uint32_t kSw128Hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+// Instruction descriptor of kind::f16 with 32-bit accumulators: dtype 0 f16, 1 bf16; *_mn 1 = MN-major.
+__host__ __device__ constexpr uint32_t f16_idesc(int bf16, int a_mn, int b_mn, int m, int n) {
+    return (1u << 4) | ((uint32_t)bf16 << 7) | ((uint32_t)bf16 << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
+           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void umma_sw128_if(uint32_t pred, uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %5};\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kSw128Hi), "r"(pred) : "memory");
+}
+// M = 256 rows over a CTA pair, issued by its first CTA: each CTA holds its 128 rows of A and half of B's columns at the same
+// places, and gets its rows of D.
+__device__ __forceinline__ void umma_sw128_pair_if(uint32_t pred, uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %5};\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %6, 0;\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kSw128Hi), "r"(pred) : "memory");
+}
+// Arrives on the barrier at this address in both CTAs of the pair once all MMAs issued so far have completed.
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+// This CTA's shared address as CTA `rank` of the cluster has it.
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 // two floats -> packed bf16 pair (first argument in the low half), round to nearest even; the second
 // form clamps negative values to zero in the same instruction
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
