@@ -49,13 +49,20 @@ struct Problem {
 };
 struct TileParams {
     Problem prob[2];
-    int n_prob, splits, stages;
+    int n_prob, splits, stages, tiles;
     uint32_t bf16;
     int* status;
 };
 
-// Up to four neighbours (row, n .. n + count - 1) of the output from their sums.
-__device__ __forceinline__ void finish4(const Epilogue& e, long long row, int n, int count, float (&v)[4]) {
+// Cycles after which a wait for a whole sum has run out: a block of 64 terms takes some hundred.
+__device__ __forceinline__ long long sum_limit(int kblocks) { return kWaitCycles + 4096ll * kblocks; }
+
+__device__ __forceinline__ void bias4(const Epilogue& e, int n, int count, float (&b)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = e.bias && i < count ? load1(e.bias, n + i, e.bias_type) : 0.0f;
+}
+// Up to four neighbours (row, n .. n + count - 1) of the output from their sums and their biases.
+__device__ __forceinline__ void finish4(const Epilogue& e, long long row, int n, int count, float (&v)[4], const float (&b)[4]) {
     float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     const bool whole = e.vec && count == 4;
     if (e.res) {
@@ -64,8 +71,8 @@ __device__ __forceinline__ void finish4(const Epilogue& e, long long row, int n,
         else
             for (int i = 0; i < 4; ++i) if (i < count) r[i] = load1(e.res, at + i, e.res_type);
     }
-    if (e.bias)
-        for (int i = 0; i < 4; ++i) if (i < count) v[i] += load1(e.bias, n + i, e.bias_type);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += b[i];
     if (e.res && e.res_first)
         for (int i = 0; i < 4; ++i) v[i] += r[i];
     if (e.pre) {
@@ -74,8 +81,7 @@ __device__ __forceinline__ void finish4(const Epilogue& e, long long row, int n,
         else
             for (int i = 0; i < 4; ++i) if (i < count) store1(e.pre, at + i, e.pre_type, v[i]);
     }
-    if (e.act != FP_ACT_NONE)
-        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], e.act);
+    act4(v, e.act);
     if (e.res && !e.res_first)
         for (int i = 0; i < 4; ++i) v[i] += r[i];
     const long long at = row * e.ld_y + n;
@@ -189,7 +195,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     }
     if (!ok && lane == 0) { atomicExch(&ctrl.abort_flag, 1); atomicExch(p.status, 1); }
     if (kb1 > kb0 && ok) {
-        ok = __all_sync(0xffffffffu, mbar_wait(done, 0, abort_flag));
+        ok = __all_sync(0xffffffffu, mbar_wait(done, 0, abort_flag, sum_limit(kb1 - kb0)));
         if (!ok && lane == 0) { atomicExch(&ctrl.abort_flag, 1); atomicExch(p.status, 1); }
     }
     tc_fence_after();
@@ -247,7 +253,9 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
                     for (int i = 0; i < 4; ++i) v[i] += u[i];
                 }
             }
-            finish4(q.e, r0 + r, n0 + c, count, v);
+            float bias[4];
+            bias4(q.e, n0 + c, count, bias);
+            finish4(q.e, r0 + r, n0 + c, count, v, bias);
         }
     }
     if (p.splits > 1) cluster_sync_all();                        // no CTA leaves while another may still read its sums
@@ -255,6 +263,168 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kCols) : "memory");
+    }
+}
+
+// ---- 256 x 256 tiles by CTA pairs -----------------------------------------------------------------------------------
+// Large products.  A 128 x 256 tile a CTA reads 48 KB of shared memory for 512 cycles of its tensor core, three quarters of what
+// the memory gives, with the epilogue's share on top; a pair of CTAs with one 256 x 256 tile (cta_group::2) holds half of B
+// each and reads 32 KB.  Pairs are persistent; accumulators of two tiles fill tensor memory, so that a tile is finished by eight
+// warps while the next one is summed.  Warp 0 copies, warp 1 of the pair's first CTA issues the MMAs, warps 4-11 finish.
+
+constexpr int kPairThreads = 384, kPairStages = 5;
+constexpr uint32_t kPairStage = 2 * 128 * 128;           // bytes of a stage in each CTA: 128 rows of A, 128 of B
+constexpr uint32_t kEpiPitch = 36;                       // words; 16-byte accesses of neighbouring lanes in different banks
+constexpr uint32_t kEpiWarp = 32 * kEpiPitch * 4;
+constexpr int kPairSmem = kPairStages * (int)kPairStage + 8 * (int)kEpiWarp + 1024;
+
+struct PairCtrl {
+    uint64_t full[kPairStages], empty[kPairStages], sums_full[2], sums_empty[2];
+    uint32_t tmem;
+    int abort_flag;
+};
+
+struct Place { const Problem* q; int i0, j0; };
+__device__ __forceinline__ Place pair_place(const TileParams& p, int tile_all) {
+    Place r;
+    r.q = &p.prob[p.n_prob > 1 && tile_all >= p.prob[1].tile0 ? 1 : 0];
+    const int tile = tile_all - r.q->tile0;
+    const int group = tile / (8 * r.q->tiles_j), in_group = tile - group * 8 * r.q->tiles_j, rows_here = min(8, r.q->tiles_i - group * 8);
+    r.i0 = (group * 8 + in_group % rows_here) * 256;
+    r.j0 = (in_group / rows_here) * 256;
+    return r;
+}
+
+__global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __grid_constant__ TileParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ PairCtrl ctrl;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
+    volatile int* abort_flag = &ctrl.abort_flag;
+    const uint32_t full0 = smem_u32(ctrl.full), empty0 = smem_u32(ctrl.empty), sums_full = smem_u32(ctrl.sums_full), sums_empty = smem_u32(ctrl.sums_empty);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            for (int i = 0; i < p.n_prob; ++i) { prefetch_map(&p.prob[i].a); prefetch_map(&p.prob[i].b); }
+            for (int s = 0; s < kPairStages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+            for (int s = 0; s < 2; ++s) { mbar_init(sums_full + 8 * s, 1); mbar_init(sums_empty + 8 * s, 16); }
+            ctrl.abort_flag = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+    } else if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl.tmem)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    tc_fence_before();
+    cluster_sync_all();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ctrl.tmem;
+    bool ok = true;
+    if (warp == 0) {
+        uint32_t stage = 0, phase = 0;
+        bool again = false;                              // whether the ring has come round
+        for (int t = pair; t < p.tiles && ok; t += pairs) {
+            const Place w = pair_place(p, t);
+            const int i0 = w.i0 + 128 * (int)rank, j0 = w.j0 + 128 * (int)rank;
+            for (int kb = 0; kb < w.q->kblocks; ++kb) {
+                if (again) ok = __all_sync(0xffffffffu, mbar_wait(empty0 + 8 * stage, phase ^ 1u, abort_flag));
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t own = full0 + 8 * stage, bar = cluster_addr(own, 0), a = base + stage * kPairStage, b = a + 128 * 128;
+                    const int k = kb * kBlockK;
+                    if (rank == 0) mbar_expect_tx(own, 2 * kPairStage);
+                    if (w.q->a_mn) {
+                        tma_load_2d_pair(a, &w.q->a, i0, k, bar);
+                        tma_load_2d_pair(a + 8192, &w.q->a, i0 + 64, k, bar);
+                    } else {
+                        tma_load_2d_pair(a, &w.q->a, k, i0, bar);
+                    }
+                    if (w.q->b_mn) {
+                        tma_load_2d_pair(b, &w.q->b, j0, k, bar);
+                        tma_load_2d_pair(b + 8192, &w.q->b, j0 + 64, k, bar);
+                    } else {
+                        tma_load_2d_pair(b, &w.q->b, k, j0, bar);
+                    }
+                }
+                __syncwarp();
+                if (++stage == kPairStages) { stage = 0; phase ^= 1u; again = true; }
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        uint32_t stage = 0, phase = 0, n = 0;
+        for (int t = pair; t < p.tiles && ok; t += pairs, ++n) {
+            const Place w = pair_place(p, t);
+            const uint32_t idesc = f16_idesc((int)p.bf16, w.q->a_mn, w.q->b_mn, 256, 256);
+            const uint32_t a_step = w.q->a_mn ? 128u : 2u, b_step = w.q->b_mn ? 128u : 2u, d = tmem + (n & 1) * 256u;
+            if (n >= 2) ok = __all_sync(0xffffffffu, mbar_wait(sums_empty + 8 * (n & 1), ((n >> 1) & 1u) ^ 1u, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            for (int kb = 0; kb < w.q->kblocks; ++kb) {
+                ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8 * stage, phase, abort_flag));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t a = base + stage * kPairStage, al = sw128_lo(a, 8192), bl = sw128_lo(a + 128 * 128, 8192), leader = elect_one();
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+                    umma_sw128_pair_if(leader, d, al + (uint32_t)s * a_step, bl + (uint32_t)s * b_step, idesc, kb || s ? 1u : 0u);
+                if (leader) {
+                    umma_commit_pair(empty0 + 8 * stage);
+                    if (kb == w.q->kblocks - 1) umma_commit_pair(sums_full + 8 * (n & 1));
+                }
+                __syncwarp();
+                if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t buf = base + kPairStages * kPairStage + (uint32_t)(warp - 4) * kEpiWarp;
+        const uint32_t put = buf + (uint32_t)lane * (kEpiPitch * 4), get = buf + (uint32_t)(lane >> 3) * (kEpiPitch * 4) + (uint32_t)(lane & 7) * 16u;
+        uint32_t n = 0;
+        for (int t = pair; t < p.tiles; t += pairs, ++n) {
+            const Place w = pair_place(p, t);
+            const Epilogue& e = w.q->e;
+            ok = __all_sync(0xffffffffu, mbar_wait(sums_full + 8 * (n & 1), (n >> 1) & 1u, abort_flag, sum_limit(w.q->kblocks)));
+            if (!ok) break;
+            tc_fence_after();
+            const int row0 = w.i0 + 128 * (int)rank + 32 * quarter + (lane >> 3);
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+                uint32_t v[32];
+                tmem_ld32(tmem + ((uint32_t)(32 * quarter) << 16) + (n & 1) * 256u + (uint32_t)(half * 128 + 32 * c), v);
+                const int col = w.j0 + half * 128 + 32 * c + (lane & 7) * 4, count = min(4, w.q->J - col);
+                float bias[4];
+                bias4(e, col, count, bias);
+                tmem_ld_wait();
+                if (c == 3) {                            // the accumulator is free for the tile after the next
+                    tc_fence_before();
+                    if (lane == 0) mbar_arrive_cluster(cluster_addr(sums_empty + 8 * (n & 1), 0));
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(put + (uint32_t)i * 16u), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
+                __syncwarp();
+                if (count > 0)
+#pragma unroll 2
+                    for (int r = 0; r < 8; ++r) {
+                        float x[4];
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "r"(get + (uint32_t)(4 * r) * (kEpiPitch * 4)) : "memory");
+                        if (row0 + 4 * r < w.q->I) finish4(e, row0 + 4 * r, col, count, x, bias);
+                    }
+                __syncwarp();
+            }
+        }
+    }
+    if (!ok && lane == 0) { atomicExch(&ctrl.abort_flag, 1); atomicExch(p.status, 1); }
+    if (*abort_flag)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);         // copies in flight land before the memory is given back
+    tc_fence_before();
+    cluster_sync_all();                                          // no CTA leaves while the other may still signal it
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
 }
 
@@ -430,43 +600,98 @@ cudaError_t launch_tiles_bn(const TileParams& p, int tiles, int smem, cudaStream
 struct Operand { const void* p; int64_t rows, cols, ld; int mn; };   // mn: rows are the sum's index
 struct Product { Operand a, b; int64_t I, J, Kc; int swap; Epilogue e; };
 
+// Fills in a launch's problems for tiles of ti x tj; false where a tensor map is refused, or there are more tiles than an index holds.
+bool lay_out(const Product* prod, int n, int ti, int tj, int box_b, int dtype, TileParams* p, int64_t* least, int64_t* most) {
+    int64_t tiles = 0;
+    *least = 1ll << 40; *most = 0;
+    for (int i = 0; i < n; ++i) {
+        const Product& r = prod[i];
+        Problem& q = p->prob[i];
+        q.I = (int)r.I; q.J = (int)r.J; q.kblocks = (int)((r.Kc + kBlockK - 1) / kBlockK);
+        q.tiles_i = (int)((r.I + ti - 1) / ti); q.tiles_j = (int)((r.J + tj - 1) / tj);
+        q.tile0 = (int)tiles;
+        tiles += (int64_t)q.tiles_i * q.tiles_j;
+        if (tiles > (1 << 27)) return false;
+        *least = std::min<int64_t>(*least, q.kblocks); *most = std::max<int64_t>(*most, q.kblocks);
+        q.a_mn = r.a.mn; q.b_mn = r.b.mn; q.swap = r.swap; q.e = r.e;
+        if (!make_map(&q.a, r.a.p, r.a.rows, r.a.cols, r.a.ld, r.a.mn ? 64 : 128, dtype) ||
+            !make_map(&q.b, r.b.p, r.b.rows, r.b.cols, r.b.ld, r.b.mn ? 64 : box_b, dtype))
+            return false;
+    }
+    p->n_prob = n; p->tiles = (int)tiles;
+    return true;
+}
+
+// Pairs of CTAs that run at once on the current device.
+int pair_room() {
+    static std::atomic<int> known[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 0; }
+    int n = known[dev].load(std::memory_order_acquire);
+    if (n == 0) {
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        cfg.gridDim = dim3(2 * 512);
+        cfg.blockDim = dim3(kPairThreads);
+        cfg.dynamicSmemBytes = kPairSmem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaFuncSetAttribute(linear_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, linear_pair_kernel, &cfg) != cudaSuccess || n <= 0) {
+            cudaGetLastError();
+            return 0;
+        }
+        known[dev].store(n, std::memory_order_release);
+    }
+    return n;
+}
+
+fp_status launched(cudaError_t e) {
+    if (e == cudaSuccess) return FP_OK;
+    cudaGetLastError();
+    return err(FP_ERR_CUDA, cudaGetErrorString(e));
+}
+
 // All products of a call in one launch.
 fp_status run_products(const Product* prod, int n, int dtype, int* status, cudaStream_t st) {
     TileParams p;
     memset(&p, 0, sizeof(p));
-    int64_t tiles = 0, kblocks = 1 << 30;
+    p.status = status; p.bf16 = dtype == FP_DTYPE_BF16; p.splits = 1;
+    int64_t least = 0, most = 0, big = 0;
+    for (int i = 0; i < n; ++i) big += prod[i].swap ? 0 : ((prod[i].I + 255) / 256) * ((prod[i].J + 255) / 256);
+    const char* refused = "fp_linear: an operand's tensor map was refused, or there are too many tiles";
+    if (big >= 64) {
+        const int room = pair_room();
+        if (room <= 0) return err(FP_ERR_CUDA, "fp_linear: no pair of blocks fits this device");
+        if (!lay_out(prod, n, 256, 256, 128, dtype, &p, &least, &most)) return err(FP_ERR_CUDA, refused);
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        cfg.gridDim = dim3((unsigned)(2 * std::min(p.tiles, room)));
+        cfg.blockDim = dim3(kPairThreads);
+        cfg.dynamicSmemBytes = kPairSmem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return launched(cudaLaunchKernelEx(&cfg, linear_pair_kernel, p));
+    }
     int bn = 128;
     if (n == 1 && prod[0].swap) bn = prod[0].J <= 16 ? 16 : prod[0].J <= 32 ? 32 : prod[0].J <= 64 ? 64 : 128;
-    for (int i = 0; i < n; ++i) {
-        const Product& r = prod[i];
-        Problem& q = p.prob[i];
-        q.I = (int)r.I; q.J = (int)r.J; q.kblocks = (int)((r.Kc + kBlockK - 1) / kBlockK);
-        q.tiles_i = (int)((r.I + 127) / 128); q.tiles_j = (int)((r.J + bn - 1) / bn);
-        if (tiles + (int64_t)q.tiles_i * q.tiles_j > (1 << 27)) return err(FP_ERR_BOUNDS, "fp_linear: more tiles than a launch takes");
-        q.tile0 = (int)tiles;
-        tiles += (int64_t)q.tiles_i * q.tiles_j;
-        kblocks = std::min<int64_t>(kblocks, q.kblocks);
-        q.a_mn = r.a.mn; q.b_mn = r.b.mn; q.swap = r.swap; q.e = r.e;
-        if (!make_map(&q.a, r.a.p, r.a.rows, r.a.cols, r.a.ld, r.a.mn ? 64 : 128, dtype) ||
-            !make_map(&q.b, r.b.p, r.b.rows, r.b.cols, r.b.ld, r.b.mn ? 64 : bn, dtype))
-            return err(FP_ERR_CUDA, "fp_linear: an operand's tensor map was refused");
-    }
-    p.n_prob = n; p.status = status; p.bf16 = dtype == FP_DTYPE_BF16;
+    if (!lay_out(prod, n, 128, bn, bn, dtype, &p, &least, &most)) return err(FP_ERR_CUDA, refused);
     const int sms = sm_count();
-    p.splits = 1;
-    while (p.splits < 8 && tiles * p.splits * 2 <= sms && kblocks >= p.splits * 4) p.splits *= 2;
-    const int stage = 128 * 128 + bn * 128, per_cta = (int)((kblocks + p.splits - 1) / p.splits);
-    int64_t most = 0;
-    for (int i = 0; i < n; ++i) most = std::max<int64_t>(most, (p.prob[i].kblocks + p.splits - 1) / p.splits);
-    (void)per_cta;
-    const int room = tiles * p.splits > sms ? kMaxSmem / 2 - 3072 : kMaxSmem - 3072;
-    p.stages = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(room / stage, 16), most));
-    const int sums = prod[0].swap ? bn * 132 * 4 : 128 * (bn + 4) * 4;
-    const int smem = std::max(p.stages * stage, sums) + 1024;
-    cudaError_t e = bn == 16 ? launch_tiles_bn<16>(p, (int)tiles, smem, st) : bn == 32 ? launch_tiles_bn<32>(p, (int)tiles, smem, st)
-                  : bn == 64 ? launch_tiles_bn<64>(p, (int)tiles, smem, st) : launch_tiles_bn<128>(p, (int)tiles, smem, st);
-    if (e != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, cudaGetErrorString(e)); }
-    return FP_OK;
+    while (p.splits < 8 && p.tiles * p.splits * 2 <= sms && least >= p.splits * 4) p.splits *= 2;
+    const int stage = 128 * 128 + bn * 128, room = p.tiles * p.splits > sms ? kMaxSmem / 2 - 3072 : kMaxSmem - 3072;
+    p.stages = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(room / stage, 16), (most + p.splits - 1) / p.splits));
+    const int sums = prod[0].swap ? bn * 132 * 4 : 128 * (bn + 4) * 4, smem = std::max(p.stages * stage, sums) + 1024;
+    return launched(bn == 16 ? launch_tiles_bn<16>(p, p.tiles, smem, st) : bn == 32 ? launch_tiles_bn<32>(p, p.tiles, smem, st)
+                    : bn == 64 ? launch_tiles_bn<64>(p, p.tiles, smem, st) : launch_tiles_bn<128>(p, p.tiles, smem, st));
 }
 
 fp_status copy_rows(const CopyJob* jobs, int n, cudaStream_t st) {

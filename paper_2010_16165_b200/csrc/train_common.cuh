@@ -98,6 +98,23 @@ __device__ __forceinline__ float act_of(float z, int act) {
         default: return z;
     }
 }
+// Four values, the choice made once for all of them.
+__device__ __forceinline__ void act4(float (&v)[4], int act) {
+    if (act == FP_ACT_NONE) return;
+    if (act == FP_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], FP_ACT_RELU);
+    } else if (act == FP_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], FP_ACT_GELU);
+    } else if (act == FP_ACT_GELU_TANH) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], FP_ACT_GELU_TANH);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], FP_ACT_SILU);
+    }
+}
 __device__ __forceinline__ float act_grad(float z, int act) {
     switch (act) {
         case FP_ACT_RELU: return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);

@@ -130,6 +130,20 @@ def test_many_tiles(B):
     forward_case(B, 2500, 5000, 136, act="gelu", pre=True)
 
 
+@pytest.mark.parametrize("M,N,K,act,out", [(2100, 2050, 520, "none", F32), (2304, 2048, 2304, "gelu", BF16), (9000, 72, 2200, "silu", F32), (136, 9000, 4100, "relu", BF16),
+                                           (4097, 515, 1030, "gelu_tanh", F32)])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_gradients_of_many_tiles(B, M, N, K, act, out, pad):
+    backward_case(B, M, N, K, act=act, out=out, pad=pad)
+
+
+def test_epilogues_of_many_tiles(B):
+    for res in (None, "after", "before"):
+        forward_case(B, 2100, 2310, 72, act="gelu", res=res, pre=True)
+        forward_case(B, 2100, 2311, 200, dtype=F16, out=F32, act="silu", res=res, pre=True, bias=F16, pad=3)
+    backward_case(B, 2100, 2052, 2049, act="relu", out=BF16, accumulate=True, dz=True)
+
+
 def test_no_rows(B):
     x, w, y = (torch.empty(s, device="cuda", dtype=torch.bfloat16) for s in ((0, 16), (8, 16), (0, 8)))
     B.fp_linear_forward(x, w, y)
