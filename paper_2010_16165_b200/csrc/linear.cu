@@ -44,57 +44,125 @@ struct Problem {
     CUtensorMap a, b;                                    // boxes of 64 k x rows, or 64 rows x 64 k (…_mn)
     int I, J, kblocks;
     int tiles_i, tiles_j, tile0;                         // this problem's tiles are tile0 ..
-    int a_mn, b_mn, swap;
+    int a_mn, b_mn;
     Epilogue e;
 };
 struct TileParams {
     Problem prob[2];
-    int n_prob, splits, stages, tiles;
+    int n_prob, stages, tiles;
     uint32_t bf16;
     int* status;
 };
 
+// Bounded wait by polling.  (A try_wait with a time hint sleeps in steps of 2.05 us here: products of some microseconds took whole
+// multiples of that.)
+__device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity, volatile int* abort_flag, long long limit_cycles = kWaitCycles) {
+    if (mbar_test_wait(bar, parity)) return true;
+    const long long t0 = clock64();
+    for (;;) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i)
+            if (mbar_test_wait(bar, parity)) return true;
+        if (*abort_flag || clock64() - t0 > limit_cycles) return false;
+    }
+}
 // Cycles after which a wait for a whole sum has run out: a block of 64 terms takes some hundred.
 __device__ __forceinline__ long long sum_limit(int kblocks) { return kWaitCycles + 4096ll * kblocks; }
 
+// A copy whose fields are in registers.  (Read where they are needed, through the pointer to the chosen problem, they were loaded
+// again for every few rows: 500 cycles a time.)
+__device__ __forceinline__ Epilogue held(const Epilogue& from) {
+    Epilogue e = from;
+    asm volatile("" : "+l"(e.y), "+l"(e.pre), "+l"(e.res), "+l"(e.bias), "+l"(e.ld_y), "+l"(e.ld_pre), "+l"(e.ld_res));
+    asm volatile("" : "+r"(e.y_type), "+r"(e.pre_type), "+r"(e.res_type), "+r"(e.bias_type), "+r"(e.act), "+r"(e.res_first), "+r"(e.vec));
+    return e;
+}
 __device__ __forceinline__ void bias4(const Epilogue& e, int n, int count, float (&b)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) b[i] = e.bias && i < count ? load1(e.bias, n + i, e.bias_type) : 0.0f;
 }
-// Up to four neighbours (row, n .. n + count - 1) of the output from their sums and their biases.
-__device__ __forceinline__ void finish4(const Epilogue& e, long long row, int n, int count, float (&v)[4], const float (&b)[4]) {
-    float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const bool whole = e.vec && count == 4;
-    if (e.res) {
-        const long long at = row * e.ld_res + n;
-        if (whole) load4(e.res, at, e.res_type, r);
-        else
-            for (int i = 0; i < 4; ++i) if (i < count) r[i] = load1(e.res, at + i, e.res_type);
+// Outputs n .. n + count - 1 (up to four) of U rows `step` apart, those below `end`, from their sums and biases.  `e` is the caller's
+// own copy: its fields stay in registers.  Where four neighbours lie aligned everywhere, all that is read is asked for before anything is written.
+template <int U>
+__device__ __forceinline__ void finish(const Epilogue& e, long long row, int step, long long end, int n, int count, float (&v)[U][4], const float (&b)[4]) {
+    if (e.vec && count == 4) {
+        float r[U][4];
+        if (e.res)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (row + u * step < end) load4(e.res, (row + u * step) * e.ld_res + n, e.res_type, r[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[u][i] += b[i];
+        if (e.res && e.res_first)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[u][i] += r[u][i];
+        if (e.pre)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (row + u * step < end) store4(e.pre, (row + u * step) * e.ld_pre + n, e.pre_type, v[u]);
+        act_all(v, e.act);
+        if (e.res && !e.res_first)
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[u][i] += r[u][i];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (row + u * step < end) store4(e.y, (row + u * step) * e.ld_y + n, e.y_type, v[u]);
+        return;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += b[i];
-    if (e.res && e.res_first)
-        for (int i = 0; i < 4; ++i) v[i] += r[i];
-    if (e.pre) {
-        const long long at = row * e.ld_pre + n;
-        if (whole) store4(e.pre, at, e.pre_type, v);
-        else
-            for (int i = 0; i < 4; ++i) if (i < count) store1(e.pre, at + i, e.pre_type, v[i]);
+    for (int u = 0; u < U; ++u) {
+        const long long at = row + u * step;
+        if (at >= end) break;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i >= count) break;
+            const float r = e.res ? load1(e.res, at * e.ld_res + n + i, e.res_type) : 0.0f;
+            float x = v[u][i] + b[i];
+            if (e.res && e.res_first) x += r;
+            if (e.pre) store1(e.pre, at * e.ld_pre + n + i, e.pre_type, x);
+            x = act_of(x, e.act);
+            if (e.res && !e.res_first) x += r;
+            store1(e.y, at * e.ld_y + n + i, e.y_type, x);
+        }
     }
-    act4(v, e.act);
-    if (e.res && !e.res_first)
-        for (int i = 0; i < 4; ++i) v[i] += r[i];
-    const long long at = row * e.ld_y + n;
-    if (whole) store4(e.y, at, e.y_type, v);
-    else
-        for (int i = 0; i < 4; ++i) if (i < count) store1(e.y, at + i, e.y_type, v[i]);
+}
+__device__ __forceinline__ void lds16(uint32_t addr, float (&v)[4]) {
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr));
+}
+__device__ __forceinline__ void lds16_cluster(uint32_t addr, float (&v)[4]) {
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr));
 }
 
-// ---- one 128 x BN tile a cluster ------------------------------------------------------------------------------------
-// `splits` CTAs share a tile's sum, a range of K blocks each; their partial sums meet in shared memory, where every
-// CTA finishes its part of the tile (the terms in the CTAs' order: one order of sums for a size).  With few rows (M <= 128)
-// the weights take the 128 rows of the tensor core's tile and the activations its BN columns: a single token then costs 16 columns instead
-// of 128 rows, and the weights' bytes are all that counts.
+// The parts of U sums that S CTAs of a cluster (first, first + every, ...) hold in their shared memory, added in that order.  All are
+// asked for at once: another CTA's memory answers after a thousand cycles.
+template <int S, int U>
+__device__ __forceinline__ void sums_of_parts(const uint32_t (&at)[U], uint32_t first, uint32_t every, float (&v)[U][4]) {
+    float part[U][S][4];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int u = 0; u < U; ++u) lds16_cluster(cluster_addr(at[u], first + every * (uint32_t)s), part[u][s]);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[u][i] = part[u][0][i];
+#pragma unroll
+            for (int s = 1; s < S; ++s) v[u][i] += part[u][s][i];
+        }
+}
+
+// ---- few rows: 128 outputs x BN rows a cluster ----------------------------------------------------------------------
+// With few rows (M <= 128) the weights take the 128 rows of the tensor core's tile and the activations its BN columns: a
+// single token costs 16 columns instead of 128 rows, and the weights' bytes are all that counts.  S CTAs share a
+// tile's sum, a range of K blocks each; their parts meet in shared memory, where every CTA finishes some rows (the terms in the
+// CTAs' order: one order of sums for a size).
 
 constexpr int kTileThreads = 256;
 struct TileCtrl {
@@ -103,11 +171,7 @@ struct TileCtrl {
     int abort_flag;
 };
 
-__device__ __forceinline__ void lds16_cluster(uint32_t addr, float (&v)[4]) {
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr) : "memory");
-}
-
-template <int BN>
+template <int BN, int S>
 __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_constant__ TileParams p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ TileCtrl ctrl;
@@ -115,15 +179,10 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     constexpr int kCols = BN < 32 ? 32 : BN;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = p.splits > 1 ? cluster_rank() : 0u;
-    const int tile_all = (int)(blockIdx.x / (unsigned)p.splits);
-    const Problem& q = p.prob[p.n_prob > 1 && tile_all >= p.prob[1].tile0 ? 1 : 0];
-    const int tile = tile_all - q.tile0;
-    // Eight row tiles at a time over all column tiles: what runs at once reads a square of the product's operands.
-    const int group = tile / (8 * q.tiles_j), in_group = tile - group * 8 * q.tiles_j;
-    const int rows_here = min(8, q.tiles_i - group * 8);
-    const int i0 = (group * 8 + in_group % rows_here) * 128, j0 = (in_group / rows_here) * BN;
-    const int kb0 = (int)((long long)q.kblocks * rank / p.splits), kb1 = (int)((long long)q.kblocks * (rank + 1) / p.splits);
+    const uint32_t rank = S > 1 ? cluster_rank() : 0u;
+    const Problem& q = p.prob[0];
+    const int tile = (int)(blockIdx.x / (unsigned)S), i0 = tile * 128;
+    const int kb0 = (int)((long long)q.kblocks * rank / S), kb1 = (int)((long long)q.kblocks * (rank + 1) / S);
     volatile int* abort_flag = &ctrl.abort_flag;
     const uint32_t full0 = smem_u32(ctrl.full), empty0 = smem_u32(ctrl.empty), done = smem_u32(&ctrl.done);
 
@@ -149,7 +208,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
         int stage = 0;
         uint32_t phase = 0;
         for (int kb = kb0; kb < kb1; ++kb) {
-            if (kb - kb0 >= p.stages) ok = __all_sync(0xffffffffu, mbar_wait(empty0 + 8 * stage, phase ^ 1u, abort_flag));
+            if (kb - kb0 >= p.stages) ok = __all_sync(0xffffffffu, mbar_poll(empty0 + 8 * stage, phase ^ 1u, abort_flag));
             if (!ok) break;
             if (elect_one()) {
                 const uint32_t bar = full0 + 8 * stage, a = base + (uint32_t)stage * kStage, b = a + 128 * 128;
@@ -161,30 +220,23 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
                 } else {
                     tma_load_2d(a, &q.a, k, i0, bar);
                 }
-                if (q.b_mn) {
-                    tma_load_2d(b, &q.b, j0, k, bar);
-                    if (BN > 64) tma_load_2d(b + 8192, &q.b, j0 + 64, k, bar);
-                } else {
-                    tma_load_2d(b, &q.b, k, j0, bar);
-                }
+                tma_load_2d(b, &q.b, k, 0, bar);
             }
             __syncwarp();
             if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
     } else if (warp == 1) {
-        const uint32_t idesc = f16_idesc((int)p.bf16, q.a_mn, q.b_mn, 128, BN);
-        const uint32_t a_step = q.a_mn ? 128u : 2u, b_step = q.b_mn ? 128u : 2u;
+        const uint32_t idesc = f16_idesc((int)p.bf16, q.a_mn, 0, 128, BN), a_step = q.a_mn ? 128u : 2u;
         int stage = 0;
         uint32_t phase = 0;
         for (int kb = kb0; kb < kb1; ++kb) {
-            ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8 * stage, phase, abort_flag));
+            ok = __all_sync(0xffffffffu, mbar_poll(full0 + 8 * stage, phase, abort_flag));
             if (!ok) break;
             tc_fence_after();
             const uint32_t a = base + (uint32_t)stage * kStage;
             const uint32_t al = sw128_lo(a, 8192), bl = sw128_lo(a + 128 * 128, 8192), leader = elect_one();
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
-                umma_sw128_if(leader, tmem, al + (uint32_t)s * a_step, bl + (uint32_t)s * b_step, idesc, kb > kb0 || s ? 1u : 0u);
+            for (int s = 0; s < 4; ++s) umma_sw128_if(leader, tmem, al + (uint32_t)s * a_step, bl + (uint32_t)s * 2u, idesc, kb > kb0 || s ? 1u : 0u);
             if (leader) {
                 umma_commit(empty0 + 8 * stage);
                 if (kb == kb1 - 1) umma_commit(done);
@@ -194,8 +246,8 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
         }
     }
     if (!ok && lane == 0) { atomicExch(&ctrl.abort_flag, 1); atomicExch(p.status, 1); }
-    if (kb1 > kb0 && ok) {
-        ok = __all_sync(0xffffffffu, mbar_wait(done, 0, abort_flag, sum_limit(kb1 - kb0)));
+    if (ok) {
+        ok = __all_sync(0xffffffffu, mbar_poll(done, 0, abort_flag, sum_limit(kb1 - kb0)));
         if (!ok && lane == 0) { atomicExch(&ctrl.abort_flag, 1); atomicExch(p.status, 1); }
     }
     tc_fence_after();
@@ -203,62 +255,42 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
         for (int i = 0; i < 200; ++i) __nanosleep(1000);         // copies in flight land before the memory is used again
     __syncthreads();                                             // every stage has been read: its memory takes the sums now
 
-    // Sums in shared memory with n along a row: [i][j], or with swap [j][i].  Pitches of 4 (mod 32) words keep 16-byte
-    // accesses of neighbouring lanes in different banks.
-    const int pitch = q.swap ? 132 : BN + 4;
+    // Sums in shared memory as rows of 128 outputs.  A pitch of 4 (mod 32) words keeps 16-byte accesses of neighbouring lanes in
+    // different banks.
+    constexpr int kPitch = 132;
+    const Epilogue e = held(q.e);
+    const int n = i0 + 4 * lane, count = min(4, q.I - n), rows = q.J;
+    float bias[4];
+    bias4(e, n, count, bias);
     {
-        const int row = (warp & 3) * 32 + lane;
+        const int col = (warp & 3) * 32 + lane;
         const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        constexpr int kChunks = BN / 8;
-#pragma unroll 1
-        for (int c = warp >> 2; c < kChunks; c += 2) {
-            uint32_t v[8];
-            tmem_ld8(taddr + (uint32_t)(8 * c), v);
-            tmem_ld_wait();
-            if (kb1 <= kb0)
-                for (int i = 0; i < 8; ++i) v[i] = 0;
-            if (q.swap) {
-                const uint32_t to = base + (uint32_t)(8 * c * pitch + row) * 4u;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + (uint32_t)(i * pitch) * 4u), "r"(v[i]) : "memory");
-            } else {
-                const uint32_t to = base + (uint32_t)(row * pitch + 8 * c) * 4u;
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
-            }
+        for (int c = 0; c < BN / 16; ++c) {
+            const int r = 8 * (2 * c + (warp >> 2));
+            if (r >= rows) break;
+            uint32_t v[8];
+            tmem_ld8(taddr + (uint32_t)r, v);
+            tmem_ld_wait();
+            const uint32_t to = base + (uint32_t)(r * kPitch + col) * 4u;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + (uint32_t)(i * kPitch) * 4u), "r"(v[i]) : "memory");
         }
     }
     tc_fence_before();
-    if (p.splits > 1) cluster_sync_all();
+    if (S > 1) cluster_sync_all();
     else __syncthreads();
-    {
-        const int r0 = q.swap ? j0 : i0, n0 = q.swap ? i0 : j0;
-        const int rows = min(q.swap ? BN : 128, (q.swap ? q.J : q.I) - r0), N = q.swap ? q.I : q.J;
-        const int per_row = (q.swap ? 128 : BN) / 4, total = rows * per_row;
-        const int from = (int)((long long)total * rank / p.splits), to = (int)((long long)total * (rank + 1) / p.splits);
-        for (int x = from + (int)threadIdx.x; x < to; x += kTileThreads) {
-            const int r = x / per_row, c = (x - r * per_row) * 4;
-            const int count = min(4, N - (n0 + c));
-            if (count <= 0) continue;
-            const uint32_t at = base + (uint32_t)(r * pitch + c) * 4u;
-            float v[4];
-            if (p.splits == 1) {
-                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(at) : "memory");
-            } else {
-                lds16_cluster(cluster_addr(at, 0), v);
-                for (int s = 1; s < p.splits; ++s) {
-                    float u[4];
-                    lds16_cluster(cluster_addr(at, (uint32_t)s), u);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] += u[i];
-                }
-            }
-            float bias[4];
-            bias4(q.e, n0 + c, count, bias);
-            finish4(q.e, r0 + r, n0 + c, count, v, bias);
+    // warp w of CTA r finishes every (8 S)th row from 8 r + w on, four outputs a lane
+    if (count > 0)
+#pragma unroll 1
+        for (int r = (int)rank * 8 + warp; r < rows; r += 8 * S) {
+            const uint32_t at = base + (uint32_t)(r * kPitch + 4 * lane) * 4u;
+            float v[1][4];
+            if (S > 1) sums_of_parts<S, 1>({at}, 0u, 1u, v);
+            else lds16(at, v[0]);
+            finish<1>(e, r, 0, rows, n, count, v, bias);
         }
-    }
-    if (p.splits > 1) cluster_sync_all();                        // no CTA leaves while another may still read its sums
+    if (S > 1) cluster_sync_all();                        // no CTA leaves while another may still read its sums
     else __syncthreads();
     if (warp == 1) {
         tc_fence_after();
@@ -295,6 +327,16 @@ __device__ __forceinline__ Place pair_place(const TileParams& p, int tile_all) {
     return r;
 }
 
+// 128 rows of an operand (from row0 on, 64 terms of the sum from k on) into this CTA's stage.
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap& map, int mn, int row0, int k, uint32_t bar) {
+    if (mn) {
+        tma_load_2d_pair(dst, &map, row0, k, bar);
+        tma_load_2d_pair(dst + 8192, &map, row0 + 64, k, bar);
+    } else {
+        tma_load_2d_pair(dst, &map, k, row0, bar);
+    }
+}
+
 __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __grid_constant__ TileParams p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ PairCtrl ctrl;
@@ -319,7 +361,6 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
     }
     tc_fence_before();
     cluster_sync_all();
-    __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctrl.tmem;
     bool ok = true;
@@ -330,24 +371,13 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
             const Place w = pair_place(p, t);
             const int i0 = w.i0 + 128 * (int)rank, j0 = w.j0 + 128 * (int)rank;
             for (int kb = 0; kb < w.q->kblocks; ++kb) {
-                if (again) ok = __all_sync(0xffffffffu, mbar_wait(empty0 + 8 * stage, phase ^ 1u, abort_flag));
+                if (again) ok = __all_sync(0xffffffffu, mbar_poll(empty0 + 8 * stage, phase ^ 1u, abort_flag));
                 if (!ok) break;
                 if (elect_one()) {
-                    const uint32_t own = full0 + 8 * stage, bar = cluster_addr(own, 0), a = base + stage * kPairStage, b = a + 128 * 128;
-                    const int k = kb * kBlockK;
+                    const uint32_t own = full0 + 8 * stage, bar = cluster_addr(own, 0), a = base + stage * kPairStage;
                     if (rank == 0) mbar_expect_tx(own, 2 * kPairStage);
-                    if (w.q->a_mn) {
-                        tma_load_2d_pair(a, &w.q->a, i0, k, bar);
-                        tma_load_2d_pair(a + 8192, &w.q->a, i0 + 64, k, bar);
-                    } else {
-                        tma_load_2d_pair(a, &w.q->a, k, i0, bar);
-                    }
-                    if (w.q->b_mn) {
-                        tma_load_2d_pair(b, &w.q->b, j0, k, bar);
-                        tma_load_2d_pair(b + 8192, &w.q->b, j0 + 64, k, bar);
-                    } else {
-                        tma_load_2d_pair(b, &w.q->b, k, j0, bar);
-                    }
+                    load_rows(a, w.q->a, w.q->a_mn, i0, kb * kBlockK, bar);
+                    load_rows(a + 128 * 128, w.q->b, w.q->b_mn, j0, kb * kBlockK, bar);
                 }
                 __syncwarp();
                 if (++stage == kPairStages) { stage = 0; phase ^= 1u; again = true; }
@@ -359,11 +389,11 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
             const Place w = pair_place(p, t);
             const uint32_t idesc = f16_idesc((int)p.bf16, w.q->a_mn, w.q->b_mn, 256, 256);
             const uint32_t a_step = w.q->a_mn ? 128u : 2u, b_step = w.q->b_mn ? 128u : 2u, d = tmem + (n & 1) * 256u;
-            if (n >= 2) ok = __all_sync(0xffffffffu, mbar_wait(sums_empty + 8 * (n & 1), ((n >> 1) & 1u) ^ 1u, abort_flag));
+            if (n >= 2) ok = __all_sync(0xffffffffu, mbar_poll(sums_empty + 8 * (n & 1), ((n >> 1) & 1u) ^ 1u, abort_flag));
             if (!ok) break;
             tc_fence_after();
             for (int kb = 0; kb < w.q->kblocks; ++kb) {
-                ok = __all_sync(0xffffffffu, mbar_wait(full0 + 8 * stage, phase, abort_flag));
+                ok = __all_sync(0xffffffffu, mbar_poll(full0 + 8 * stage, phase, abort_flag));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t a = base + stage * kPairStage, al = sw128_lo(a, 8192), bl = sw128_lo(a + 128 * 128, 8192), leader = elect_one();
@@ -371,8 +401,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
                 for (int s = 0; s < 4; ++s)
                     umma_sw128_pair_if(leader, d, al + (uint32_t)s * a_step, bl + (uint32_t)s * b_step, idesc, kb || s ? 1u : 0u);
                 if (leader) {
-                    umma_commit_pair(empty0 + 8 * stage);
-                    if (kb == w.q->kblocks - 1) umma_commit_pair(sums_full + 8 * (n & 1));
+                    umma_commit_pair(empty0 + 8 * stage, 0);
+                    if (kb == w.q->kblocks - 1) umma_commit_pair(sums_full + 8 * (n & 1), 0);
                 }
                 __syncwarp();
                 if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
@@ -385,8 +415,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
         uint32_t n = 0;
         for (int t = pair; t < p.tiles; t += pairs, ++n) {
             const Place w = pair_place(p, t);
-            const Epilogue& e = w.q->e;
-            ok = __all_sync(0xffffffffu, mbar_wait(sums_full + 8 * (n & 1), (n >> 1) & 1u, abort_flag, sum_limit(w.q->kblocks)));
+            const Epilogue e = held(w.q->e);
+            ok = __all_sync(0xffffffffu, mbar_poll(sums_full + 8 * (n & 1), (n >> 1) & 1u, abort_flag, sum_limit(w.q->kblocks)));
             if (!ok) break;
             tc_fence_after();
             const int row0 = w.i0 + 128 * (int)rank + 32 * quarter + (lane >> 3);
@@ -407,11 +437,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(put + (uint32_t)i * 16u), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
                 __syncwarp();
                 if (count > 0)
-#pragma unroll 2
-                    for (int r = 0; r < 8; ++r) {
-                        float x[4];
-                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "r"(get + (uint32_t)(4 * r) * (kEpiPitch * 4)) : "memory");
-                        if (row0 + 4 * r < w.q->I) finish4(e, row0 + 4 * r, col, count, x, bias);
+#pragma unroll 1
+                    for (int r = 0; r < 8; r += 4) {
+                        float x[4][4];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) lds16(get + (uint32_t)(4 * (r + u)) * (kEpiPitch * 4), x[u]);
+                        finish<4>(e, row0 + 4 * r, 4, w.q->I, col, count, x, bias);
                     }
                 __syncwarp();
             }
@@ -425,6 +456,143 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+// ---- 256 x 256 tiles with the sum split over pairs ----------------------------------------------------------------------
+// Products of fewer tiles than there are pairs: S pairs (a cluster of 2 S CTAs) share a tile's sum, as with few rows.
+// An SM takes 64 bytes a cycle from L2, so tiles are what counts: 32 KB a K block for 512 cycles of the tensor cores here; 128 x 128
+// tiles of single CTAs need the same 32 KB for 256 cycles' work and ran at half the rate however they were spread.
+
+constexpr int kSplitThreads = 256, kSumPitch = 260;      // words of a row of sums: 16-byte accesses of neighbouring lanes in different banks
+constexpr int kSplitSmem = kPairStages * (int)kPairStage + 1024;
+static_assert(128 * kSumPitch * 4 <= kPairStages * (int)kPairStage, "the sums take the stages' memory");
+
+template <int S>
+__global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __grid_constant__ TileParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ PairCtrl ctrl;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank(), half = rank & 1u, first = rank & ~1u;      // this CTA's place in its pair, and the pair's first CTA
+    const int split = (int)(rank >> 1);
+    const Place w = pair_place(p, (int)(blockIdx.x / (unsigned)(2 * S)));
+    const Problem& q = *w.q;
+    const int i0 = w.i0 + 128 * (int)half;
+    const int kb0 = (int)((long long)q.kblocks * split / S), kb1 = (int)((long long)q.kblocks * (split + 1) / S);
+    volatile int* abort_flag = &ctrl.abort_flag;
+    const uint32_t full0 = smem_u32(ctrl.full), empty0 = smem_u32(ctrl.empty), done = smem_u32(ctrl.sums_full);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            prefetch_map(&q.a);
+            prefetch_map(&q.b);
+            for (int s = 0; s < kPairStages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+            mbar_init(done, 1);
+            ctrl.abort_flag = 0;
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+    } else if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl.tmem)), "r"(256u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    tc_fence_before();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem = ctrl.tmem;
+    bool ok = true;
+    if (warp == 0) {
+        uint32_t stage = 0, phase = 0;
+        const int j0 = w.j0 + 128 * (int)half;
+        for (int kb = kb0; kb < kb1; ++kb) {
+            if (kb - kb0 >= kPairStages) ok = __all_sync(0xffffffffu, mbar_poll(empty0 + 8 * stage, phase ^ 1u, abort_flag));
+            if (!ok) break;
+            if (elect_one()) {
+                const uint32_t own = full0 + 8 * stage, bar = cluster_addr(own, first), a = base + stage * kPairStage;
+                if (half == 0) mbar_expect_tx(own, 2 * kPairStage);
+                load_rows(a, q.a, q.a_mn, i0, kb * kBlockK, bar);
+                load_rows(a + 128 * 128, q.b, q.b_mn, j0, kb * kBlockK, bar);
+            }
+            __syncwarp();
+            if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+        }
+    } else if (warp == 1 && half == 0) {
+        uint32_t stage = 0, phase = 0;
+        const uint32_t idesc = f16_idesc((int)p.bf16, q.a_mn, q.b_mn, 256, 256), a_step = q.a_mn ? 128u : 2u, b_step = q.b_mn ? 128u : 2u;
+        for (int kb = kb0; kb < kb1; ++kb) {
+            ok = __all_sync(0xffffffffu, mbar_poll(full0 + 8 * stage, phase, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t a = base + stage * kPairStage, al = sw128_lo(a, 8192), bl = sw128_lo(a + 128 * 128, 8192), leader = elect_one();
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                umma_sw128_pair_if(leader, tmem, al + (uint32_t)s * a_step, bl + (uint32_t)s * b_step, idesc, kb > kb0 || s ? 1u : 0u);
+            if (leader) {
+                umma_commit_pair(empty0 + 8 * stage, first);
+                if (kb == kb1 - 1) umma_commit_pair(done, first);
+            }
+            __syncwarp();
+            if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+        }
+    }
+    if (!ok && lane == 0) { atomicExch(&ctrl.abort_flag, 1); atomicExch(p.status, 1); }
+    if (ok) {
+        ok = __all_sync(0xffffffffu, mbar_poll(done, 0, abort_flag, sum_limit(kb1 - kb0)));
+        if (!ok && lane == 0) { atomicExch(&ctrl.abort_flag, 1); atomicExch(p.status, 1); }
+    }
+    tc_fence_after();
+    if (*abort_flag)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);         // copies in flight land before the memory is used again
+    __syncthreads();                                             // every stage has been read: its memory takes the sums now
+    {
+        const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * 128);
+        const uint32_t to = base + (uint32_t)(((warp & 3) * 32 + lane) * kSumPitch + (warp >> 2) * 128) * 4u;
+#pragma unroll 2
+        for (int c = 0; c < 4; ++c) {
+            uint32_t v[32];
+            tmem_ld32(taddr + (uint32_t)(32 * c), v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (uint32_t)(32 * c + 4 * i) * 4u), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
+        }
+    }
+    tc_fence_before();
+    if (S > 1) cluster_sync_all();
+    else __syncthreads();
+    {
+        // Row r of this half of the tile is finished by warp r % 8 of pair (r / 8) % S, four outputs a lane and 128 further four more.
+        const Epilogue e = held(q.e);
+        const int rows = min(128, q.I - i0), step = 8 * S;
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+            const int n = w.j0 + 128 * c + 4 * lane, count = min(4, q.J - n);
+            if (count <= 0) break;
+            float bias[4];
+            bias4(e, n, count, bias);
+            const uint32_t at0 = base + (uint32_t)(128 * c + 4 * lane) * 4u;
+            constexpr int U = S == 1 ? 4 : 8 / S;
+#pragma unroll 1
+            for (int r = split * 8 + warp; r < rows; r += U * step) {
+                float v[U][4];
+                uint32_t at[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) at[u] = at0 + (uint32_t)(min(r + u * step, rows - 1) * kSumPitch) * 4u;
+                if (S > 1) {
+                    sums_of_parts<S, U>(at, half, 2u, v);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) lds16(at[u], v[u]);
+                }
+                finish<U>(e, (long long)i0 + r, step, (long long)i0 + rows, n, count, v, bias);
+            }
+        }
+    }
+    __syncwarp();
+    cluster_sync_all();                                          // no CTA leaves while another may still read its sums or signal it
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
     }
 }
 
@@ -577,33 +745,25 @@ int* status_word(int dev) {
     return p;
 }
 
-template <int BN>
-cudaError_t launch_tiles_bn(const TileParams& p, int tiles, int smem, cudaStream_t st) {
-    // (set at every call, as it is kept for each device by itself and costs nothing beside the launch)
-    cudaError_t e = cudaFuncSetAttribute(linear_tile_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem - (int)sizeof(TileCtrl) - 64);
+// Shared memory that a kernel may have, asked for once on each device.
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, std::atomic<unsigned long long>* done) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3((unsigned)(tiles * p.splits));
-    cfg.blockDim = dim3(kTileThreads);
-    cfg.dynamicSmemBytes = (size_t)smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)p.splits;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, linear_tile_kernel<BN>, p);
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (dev < 64 && (done->load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) done->fetch_or(bit, std::memory_order_release);
+    return e;
 }
 
 struct Operand { const void* p; int64_t rows, cols, ld; int mn; };   // mn: rows are the sum's index
 struct Product { Operand a, b; int64_t I, J, Kc; int swap; Epilogue e; };
 
 // Fills in a launch's problems for tiles of ti x tj; false where a tensor map is refused, or there are more tiles than an index holds.
-bool lay_out(const Product* prod, int n, int ti, int tj, int box_b, int dtype, TileParams* p, int64_t* least, int64_t* most) {
+bool lay_out(const Product* prod, int n, int ti, int tj, int dtype, TileParams* p) {
     int64_t tiles = 0;
-    *least = 1ll << 40; *most = 0;
     for (int i = 0; i < n; ++i) {
         const Product& r = prod[i];
         Problem& q = p->prob[i];
@@ -612,42 +772,48 @@ bool lay_out(const Product* prod, int n, int ti, int tj, int box_b, int dtype, T
         q.tile0 = (int)tiles;
         tiles += (int64_t)q.tiles_i * q.tiles_j;
         if (tiles > (1 << 27)) return false;
-        *least = std::min<int64_t>(*least, q.kblocks); *most = std::max<int64_t>(*most, q.kblocks);
-        q.a_mn = r.a.mn; q.b_mn = r.b.mn; q.swap = r.swap; q.e = r.e;
+        q.a_mn = r.a.mn; q.b_mn = r.b.mn; q.e = r.e;
         if (!make_map(&q.a, r.a.p, r.a.rows, r.a.cols, r.a.ld, r.a.mn ? 64 : 128, dtype) ||
-            !make_map(&q.b, r.b.p, r.b.rows, r.b.cols, r.b.ld, r.b.mn ? 64 : box_b, dtype))
+            !make_map(&q.b, r.b.p, r.b.rows, r.b.cols, r.b.ld, r.b.mn ? 64 : std::min(tj, 128), dtype))
             return false;
     }
     p->n_prob = n; p->tiles = (int)tiles;
     return true;
 }
 
-// Pairs of CTAs that run at once on the current device.
-int pair_room() {
-    static std::atomic<int> known[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 0; }
-    int n = known[dev].load(std::memory_order_acquire);
-    if (n == 0) {
-        cudaLaunchConfig_t cfg;
-        memset(&cfg, 0, sizeof(cfg));
-        cfg.gridDim = dim3(2 * 512);
-        cfg.blockDim = dim3(kPairThreads);
-        cfg.dynamicSmemBytes = kPairSmem;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = 2;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        if (cudaFuncSetAttribute(linear_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(&n, linear_pair_kernel, &cfg) != cudaSuccess || n <= 0) {
-            cudaGetLastError();
-            return 0;
-        }
-        known[dev].store(n, std::memory_order_release);
-    }
-    return n;
+template <typename K>
+cudaError_t launch_clusters(K kernel, const TileParams& p, int blocks, int threads, int smem, int cluster, cudaStream_t st) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+template <int BN, int S>
+cudaError_t launch_tiles_of(const TileParams& p, int smem, cudaStream_t st) {
+    static std::atomic<unsigned long long> done;
+    const cudaError_t e = allow_smem(linear_tile_kernel<BN, S>, kMaxSmem - (int)sizeof(TileCtrl) - 64, &done);
+    return e != cudaSuccess ? e : launch_clusters(linear_tile_kernel<BN, S>, p, p.tiles * S, kTileThreads, smem, S, st);
+}
+template <int BN>
+cudaError_t launch_tiles(const TileParams& p, int splits, int smem, cudaStream_t st) {
+    return splits == 1 ? launch_tiles_of<BN, 1>(p, smem, st) : splits == 2 ? launch_tiles_of<BN, 2>(p, smem, st)
+         : splits == 4 ? launch_tiles_of<BN, 4>(p, smem, st) : launch_tiles_of<BN, 8>(p, smem, st);
+}
+template <int S>
+cudaError_t launch_split(const TileParams& p, cudaStream_t st) {
+    static std::atomic<unsigned long long> done;
+    const cudaError_t e = allow_smem(linear_split_kernel<S>, kSplitSmem, &done);
+    return e != cudaSuccess ? e : launch_clusters(linear_split_kernel<S>, p, 2 * p.tiles * S, kSplitThreads, kSplitSmem, 2 * S, st);
 }
 
 fp_status launched(cudaError_t e) {
@@ -656,42 +822,37 @@ fp_status launched(cudaError_t e) {
     return err(FP_ERR_CUDA, cudaGetErrorString(e));
 }
 
-// All products of a call in one launch.
+// Up to two products in one launch.
 fp_status run_products(const Product* prod, int n, int dtype, int* status, cudaStream_t st) {
     TileParams p;
     memset(&p, 0, sizeof(p));
-    p.status = status; p.bf16 = dtype == FP_DTYPE_BF16; p.splits = 1;
-    int64_t least = 0, most = 0, big = 0;
-    for (int i = 0; i < n; ++i) big += prod[i].swap ? 0 : ((prod[i].I + 255) / 256) * ((prod[i].J + 255) / 256);
+    p.status = status; p.bf16 = dtype == FP_DTYPE_BF16;
     const char* refused = "fp_linear: an operand's tensor map was refused, or there are too many tiles";
-    if (big >= 64) {
-        const int room = pair_room();
-        if (room <= 0) return err(FP_ERR_CUDA, "fp_linear: no pair of blocks fits this device");
-        if (!lay_out(prod, n, 256, 256, 128, dtype, &p, &least, &most)) return err(FP_ERR_CUDA, refused);
-        cudaLaunchConfig_t cfg;
-        memset(&cfg, 0, sizeof(cfg));
-        cfg.gridDim = dim3((unsigned)(2 * std::min(p.tiles, room)));
-        cfg.blockDim = dim3(kPairThreads);
-        cfg.dynamicSmemBytes = kPairSmem;
-        cfg.stream = st;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = 2;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        return launched(cudaLaunchKernelEx(&cfg, linear_pair_kernel, p));
-    }
-    int bn = 128;
-    if (n == 1 && prod[0].swap) bn = prod[0].J <= 16 ? 16 : prod[0].J <= 32 ? 32 : prod[0].J <= 64 ? 64 : 128;
-    if (!lay_out(prod, n, 128, bn, bn, dtype, &p, &least, &most)) return err(FP_ERR_CUDA, refused);
     const int sms = sm_count();
-    while (p.splits < 8 && p.tiles * p.splits * 2 <= sms && least >= p.splits * 4) p.splits *= 2;
-    const int stage = 128 * 128 + bn * 128, room = p.tiles * p.splits > sms ? kMaxSmem / 2 - 3072 : kMaxSmem - 3072;
-    p.stages = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(room / stage, 16), (most + p.splits - 1) / p.splits));
-    const int sums = prod[0].swap ? bn * 132 * 4 : 128 * (bn + 4) * 4, smem = std::max(p.stages * stage, sums) + 1024;
-    return launched(bn == 16 ? launch_tiles_bn<16>(p, p.tiles, smem, st) : bn == 32 ? launch_tiles_bn<32>(p, p.tiles, smem, st)
-                    : bn == 64 ? launch_tiles_bn<64>(p, p.tiles, smem, st) : launch_tiles_bn<128>(p, p.tiles, smem, st));
+    int splits = 1;
+    if (prod[0].swap) {
+        const int bn = prod[0].J <= 16 ? 16 : prod[0].J <= 32 ? 32 : prod[0].J <= 64 ? 64 : 128;
+        if (!lay_out(prod, n, 128, bn, dtype, &p)) return err(FP_ERR_CUDA, refused);
+        const int kblocks = p.prob[0].kblocks;
+        while (splits < 8 && p.tiles * splits * 2 <= sms && kblocks >= splits * 4) splits *= 2;
+        const int stage = 128 * 128 + bn * 128, room = p.tiles * splits > sms ? kMaxSmem / 2 - 3072 : kMaxSmem - 3072;
+        p.stages = std::min(std::min(room / stage, 16), (kblocks + splits - 1) / splits);
+        const int smem = std::max(p.stages * stage, bn * 132 * 4) + 1024;
+        return launched(bn == 16 ? launch_tiles<16>(p, splits, smem, st) : bn == 32 ? launch_tiles<32>(p, splits, smem, st)
+                        : bn == 64 ? launch_tiles<64>(p, splits, smem, st) : launch_tiles<128>(p, splits, smem, st));
+    }
+    if (!lay_out(prod, n, 256, 256, dtype, &p)) return err(FP_ERR_CUDA, refused);
+    if (p.tiles > sms / 2) {
+        static std::atomic<unsigned long long> done;
+        const cudaError_t e = allow_smem(linear_pair_kernel, kPairSmem, &done);
+        return launched(e != cudaSuccess ? e : launch_clusters(linear_pair_kernel, p, 2 * (sms / 2), kPairThreads, kPairSmem, 2, st));
+    }
+    int kblocks = p.prob[0].kblocks;
+    if (n > 1) kblocks = std::min(kblocks, p.prob[1].kblocks);
+    // A cluster lies within a group of SMs: of 148, clusters of four CTAs reach 132, of eight 120 - and one cluster too many takes as
+    // long as all others (1024 x 1024 x 1024 in 16 clusters of eight 19.8 us).
+    while (splits < 4 && 2 * p.tiles * splits * 2 <= (splits == 1 ? sms * 132 / 148 : sms * 120 / 148) && kblocks >= splits * 4) splits *= 2;
+    return launched(splits == 1 ? launch_split<1>(p, st) : splits == 2 ? launch_split<2>(p, st) : launch_split<4>(p, st));
 }
 
 fp_status copy_rows(const CopyJob* jobs, int n, cudaStream_t st) {
@@ -921,21 +1082,26 @@ extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work
     if (a->d_dx) {
         Product& r = p[n++];
         const Operand odz = {dz, a->M, a->N, ld_dz, 0}, ow = {wt, a->N, a->K, ld_w, 1};
-        r.swap = a->M <= 128 && !a->d_dw;
+        r.swap = a->M <= 128;
         r.a = r.swap ? ow : odz; r.b = r.swap ? odz : ow;
         r.I = r.swap ? a->K : a->M; r.J = r.swap ? a->M : a->K; r.Kc = a->N;
         r.e.y = a->d_dx; r.e.ld_y = a->ld_dx; r.e.y_type = a->dtype;
         r.e.vec = aligned4(a->d_dx, a->ld_dx, a->dtype, a->M);
+        if (r.swap) {
+            if ((s = run_products(p, 1, a->dtype, status, st)) != FP_OK) return s;
+            n = 0;
+        }
     }
     if (a->d_dw) {
         Product& r = p[n++];
+        r.swap = 0;
         r.a = {dz, a->M, a->N, ld_dz, 1}; r.b = {x, a->M, a->K, ld_x, 1};
         r.I = a->N; r.J = a->K; r.Kc = a->M;
         r.e.y = a->d_dw; r.e.ld_y = a->ld_dw; r.e.y_type = a->dw_dtype;
         if (a->accumulate) { r.e.res = a->d_dw; r.e.ld_res = a->ld_dw; r.e.res_type = a->dw_dtype; }
         r.e.vec = aligned4(a->d_dw, a->ld_dw, a->dw_dtype, a->N);
     }
-    return run_products(p, n, a->dtype, status, st);
+    return n ? run_products(p, n, a->dtype, status, st) : FP_OK;
 }
 
 extern "C" fp_status fp_linear_status(int32_t* out) {

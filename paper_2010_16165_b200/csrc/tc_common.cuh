@@ -195,10 +195,11 @@ __device__ __forceinline__ void umma_sw128_pair_if(uint32_t pred, uint32_t d_tme
         "@q tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, p;\n\t}"
         ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kSw128Hi), "r"(pred) : "memory");
 }
-// Arrives on the barrier at this address in both CTAs of the pair once all MMAs issued so far have completed.
-__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
+// Arrives on the barrier at this address in both CTAs of the pair, whose first CTA has number `first` in the cluster, once all MMAs
+// issued so far have completed.
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint32_t first) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((uint16_t)3) : "memory");
+                 ::"r"(bar), "h"((uint16_t)(3u << first)) : "memory");
 }
 // This CTA's shared address as CTA `rank` of the cluster has it.
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {

@@ -98,22 +98,20 @@ __device__ __forceinline__ float act_of(float z, int act) {
         default: return z;
     }
 }
-// Four values, the choice made once for all of them.
-__device__ __forceinline__ void act4(float (&v)[4], int act) {
-    if (act == FP_ACT_NONE) return;
-    if (act == FP_ACT_RELU) {
+// Rows of four values, the choice made once for all of them.
+template <int ACT, int U>
+__device__ __forceinline__ void act_rows(float (&v)[U][4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], FP_ACT_RELU);
-    } else if (act == FP_ACT_GELU) {
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], FP_ACT_GELU);
-    } else if (act == FP_ACT_GELU_TANH) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], FP_ACT_GELU_TANH);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], FP_ACT_SILU);
-    }
+        for (int i = 0; i < 4; ++i) v[u][i] = act_of(v[u][i], ACT);
+}
+template <int U>
+__device__ __forceinline__ void act_all(float (&v)[U][4], int act) {
+    if (act == FP_ACT_RELU) act_rows<FP_ACT_RELU>(v);
+    else if (act == FP_ACT_GELU) act_rows<FP_ACT_GELU>(v);
+    else if (act == FP_ACT_GELU_TANH) act_rows<FP_ACT_GELU_TANH>(v);
+    else if (act == FP_ACT_SILU) act_rows<FP_ACT_SILU>(v);
 }
 __device__ __forceinline__ float act_grad(float z, int act) {
     switch (act) {
