@@ -4,17 +4,19 @@
 // d loss / dx_j = exp(x_j - m) / s - e / C - (1 - e) [j = y].
 //
 // Memory bound: logits are read once and the gradient written once.  The gradient needs s, so a row has to be kept between the
-// two: in registers.  A thread has up to kMaxVecs 16-byte vectors of its row, and a row is shared by as many threads as
-// that takes: 8, 32 .. 1024, or 4 or 8 blocks of 1024 as a cluster (half a million logits of 16 bits) whose maxima and sums meet in shared memory.  Longer rows, and rows
-// whose starts are not aligned to 16 bytes, are read twice by the same number of threads (the second time out of L2 where it
-// holds them).
+// two: in registers, up to eight 16-byte units a thread, by as many threads as that takes: 8, 32 .. 512, or 2, 4 or 8 blocks of
+// 512 as a cluster, whose maxima and sums meet in shared memory; more, smaller blocks an SM let one row's copies run beside
+// another's arithmetic.  Units lie at 16-byte boundaries of memory, whatever the row starts at: its first and last
+// one may be partial.  Where the gradient's row lies otherwise than the logits', a warp passes it through shared memory and writes
+// elements, neighbours by neighbouring lanes.  Rows longer than 32768 units are read twice.
+// Two exponentials and some ten instructions an element are close to what the memory leaves time for, hence: the maximum of 16-bit logits is
+// taken two at a time, what is missing of a partial unit counts as -inf instead of being asked for everywhere, and the label's own
+// element is written a second time instead of every element being compared with it.
 #include "train_common.cuh"
 #include "tc_common.cuh"
 
 #include <math.h>
 #include <string.h>
-
-#include <algorithm>
 
 namespace fp {
 namespace {
@@ -32,51 +34,85 @@ struct LossParams {
     float smoothing, scale;
 };
 
+// 2^x; results below 2^-126 are 0.  e^d as 2^(d log2 e): d = x - m is exact or rounded once, so large logits cost nothing.
+__device__ __forceinline__ float exp2_of(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float exp_of(float d) { return exp2_of(d * 1.4426950408889634f); }
+
 // Maximum, sum of exponentials below it, and plain sum of a part of a row.  A part of -inf alone has m = -inf, s = 0.
 struct Part { float m, s, t; };
 __device__ __forceinline__ Part join(const Part& a, const Part& b) {
     Part r;
     r.m = fmaxf(a.m, b.m);
     r.t = a.t + b.t;
-    r.s = (a.m == r.m ? a.s : a.s * __expf(a.m - r.m)) + (b.m == r.m ? b.s : b.s * __expf(b.m - r.m));
+    r.s = (a.m == r.m ? a.s : a.s * exp_of(a.m - r.m)) + (b.m == r.m ? b.s : b.s * exp_of(b.m - r.m));
     return r;
 }
 
-template <int DT> struct Elems { static constexpr int kPer = DT == FP_DTYPE_F32 ? 4 : 8; };      // elements of 16 bytes
-template <int DT>
-__device__ __forceinline__ float elem(const uint4& u, int i) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-    if (DT == FP_DTYPE_F32) return __uint_as_float(w[i]);
-    return to_f32((uint16_t)(w[i >> 1] >> (16 * (i & 1))), DT);
-}
-template <int DT>
-__device__ __forceinline__ uint4 vec_of(const float* v) {
-    if (DT == FP_DTYPE_F32) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-    return make_uint4(to_16x2(v[0], v[1], DT), to_16x2(v[2], v[3], DT), to_16x2(v[4], v[5], DT), to_16x2(v[6], v[7], DT));
-}
+// 16 bytes of a row.
+template <int DT> struct Unit {
+    static constexpr int E = DT == FP_DTYPE_F32 ? 4 : 8;
+    __device__ __forceinline__ static float get(const uint4& u, int i) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        if (DT == FP_DTYPE_F32) return __uint_as_float(w[i]);
+        if (DT == FP_DTYPE_BF16) return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+        return __half2float(__ushort_as_half((uint16_t)(w[i >> 1] >> (16 * (i & 1)))));
+    }
+    __device__ __forceinline__ static uint4 make(const float (&v)[8]) {
+        if (DT == FP_DTYPE_F32) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        return make_uint4(to_16x2(v[0], v[1], DT), to_16x2(v[2], v[3], DT), to_16x2(v[4], v[5], DT), to_16x2(v[6], v[7], DT));
+    }
+    __device__ __forceinline__ static uint4 nothing() {
+        const float v[8] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        return make(v);
+    }
+    __device__ __forceinline__ static uint4 load(const void* x, long long at) {
+        return __ldcs(reinterpret_cast<const uint4*>(static_cast<const char*>(x) + at * (16 / E)));
+    }
+    __device__ __forceinline__ static void store(void* x, long long at, const uint4& u) {
+        __stcs(reinterpret_cast<uint4*>(static_cast<char*>(x) + at * (16 / E)), u);
+    }
+    // the larger of two units, element by element (NaN gives way, as in fmaxf)
+    __device__ __forceinline__ static uint4 larger(const uint4& a, const uint4& b) {
+        if (DT == FP_DTYPE_F32) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = fmaxf(get(a, i), get(b, i));
+            return make(v);
+        }
+        return make_uint4(pair(a.x, b.x), pair(a.y, b.y), pair(a.z, b.z), pair(a.w, b.w));
+    }
+    __device__ __forceinline__ static uint32_t pair(uint32_t a, uint32_t b) {
+        uint32_t r;
+        if (DT == FP_DTYPE_BF16) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    // elements of memory from the last 16-byte boundary to this row's start
+    __device__ __forceinline__ static int shift(const void* x, long long at) {
+        return (int)((reinterpret_cast<uintptr_t>(x) + (uintptr_t)at * (16 / E)) & 15) / (16 / E);
+    }
+};
 
-// What a thread adds up of its row: the maximum of its elements first, then the sum below it.
+// What a thread has of its row in the first `used` of its units: the maximum first, then the sum below it.
 template <int DT, int V>
-__device__ __forceinline__ Part part_of(const uint4 (&u)[V], int vecs, int count_last) {
-    constexpr int E = Elems<DT>::kPer;
+__device__ __forceinline__ Part part_of(const uint4 (&u)[V], int used) {
+    typedef Unit<DT> U;
+    uint4 top = u[0];
+#pragma unroll
+    for (int k = 1; k < V; ++k) top = U::larger(top, u[k]);
     Part a = {-INFINITY, 0.0f, 0.0f};
 #pragma unroll
-    for (int k = 0; k < V; ++k)
-        if (k < vecs)
-#pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (k < vecs - 1 || i < count_last) a.m = fmaxf(a.m, elem<DT>(u[k], i));
+    for (int i = 0; i < U::E; ++i) a.m = fmaxf(a.m, U::get(top, i));
     const float m = a.m == -INFINITY ? 0.0f : a.m;       // (of -inf alone every exponential below is 0)
 #pragma unroll
     for (int k = 0; k < V; ++k)
-        if (k < vecs)
+        if (k < used)
 #pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (k < vecs - 1 || i < count_last) {
-                    const float x = elem<DT>(u[k], i);
-                    a.t += x;
-                    a.s += __expf(x - m);
-                }
+            for (int i = 0; i < U::E; ++i) a.s += exp_of(U::get(u[k], i) - m);
     return a;
 }
 
@@ -105,15 +141,16 @@ __device__ __forceinline__ Part join_all(Part a, Part* shared) {
     if (CL == 1) return a;
     if (threadIdx.x == 0) shared[32] = a;
     tc::cluster_sync_all();
-    Part r;
-#pragma unroll 1
+    Part all[CL];
+#pragma unroll
     for (int c = 0; c < CL; ++c) {
         const uint32_t at = tc::cluster_addr(tc::smem_u32(&shared[32]), (uint32_t)c);
-        Part b;
-        asm volatile("ld.shared::cluster.f32 %0, [%3];\n\tld.shared::cluster.f32 %1, [%3+4];\n\tld.shared::cluster.f32 %2, [%3+8];" : "=f"(b.m), "=f"(b.s), "=f"(b.t) : "r"(at));
-        r = c ? join(r, b) : b;
+        asm volatile("ld.shared::cluster.f32 %0, [%3];\n\tld.shared::cluster.f32 %1, [%3+4];\n\tld.shared::cluster.f32 %2, [%3+8];" : "=f"(all[c].m), "=f"(all[c].s), "=f"(all[c].t) : "r"(at));
     }
-    return r;
+    a = all[0];
+#pragma unroll
+    for (int c = 1; c < CL; ++c) a = join(a, all[c]);
+    return a;
 }
 
 struct Row { long long label; float g, label_x; bool ignored, bad; };
@@ -133,100 +170,146 @@ __device__ __forceinline__ float loss_of(const LossParams& p, const Row& r, cons
     return r.ignored ? 0.0f : r.bad ? NAN : l;
 }
 
-// Rows in registers: V vectors a thread, G threads a row (G < 256: several rows a block of 256), CL blocks.
+// The gradient's element from x: what is common to a row is in here.
+struct Slope {
+    float m, scale, off;                                 // scale (e^(x - m)) - off
+    __device__ __forceinline__ Slope(const LossParams& p, const Row& r, const Part& a) {
+        m = a.m;
+        scale = r.bad ? NAN : r.g / a.s;
+        off = r.g * (p.smoothing / (float)p.C);
+    }
+    __device__ __forceinline__ float operator()(float x) const { return fmaf(exp_of(x - m), scale, -off); }
+};
+
+// Rows in registers: V units a thread, G threads a row (G < 256: several rows a block of 256), CL blocks.
 template <int DT, int G, int V, int CL>
-__global__ void __launch_bounds__(G < 256 ? 256 : G) cross_entropy_kernel(const LossParams p) {
-    constexpr int E = Elems<DT>::kPer, B = G < 256 ? 256 : G;
+__global__ void __launch_bounds__(G < 256 ? 256 : G, G < 512 ? 4 : 2) cross_entropy_kernel(const LossParams p) {
+    typedef Unit<DT> U;
+    constexpr int E = U::E, B = G < 256 ? 256 : G, kStep = G * CL;
     __shared__ Part shared[33];
+    __shared__ uint4 staged[G < 32 ? 1 : B];
     const long long row = CL > 1 ? (long long)(blockIdx.x / CL) : (long long)blockIdx.x * (B / G) + threadIdx.x / G;
-    const bool there = row < p.rows;                     // (all threads of a row, and of a block of several warps a row, agree)
-    const int t = (CL > 1 ? (int)(blockIdx.x % CL) * G : 0) + (int)threadIdx.x % G;
-    const int all = (p.C + E - 1) / E, vecs = there && t < all ? (all - 1 - t) / (G * CL) + 1 : 0;
-    const int last = t + (vecs - 1) * G * CL, count_last = vecs > 0 ? min(E, p.C - last * E) : 0;
-    Row r = {};
+    const bool there = row < p.rows;                     // (all threads of a row agree, and of a block of one row)
+    const int t = (CL > 1 ? (int)(blockIdx.x % CL) * G : 0) + (int)threadIdx.x % G, lane = threadIdx.x & 31;
+    const long long at = row * p.ld_x, to = row * p.ld_dx;
+    // unit n has elements n E - shift .. of the row; the first and the last may reach over its ends
+    const int shift = U::shift(p.x, at), units = there ? (p.C + shift + E - 1) / E : 0, used = (units + kStep - 1) / kStep;
     uint4 u[V];
+    auto partial = [&](int n) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < E && (unsigned)(n * E - shift + i) < (unsigned)p.C ? load1(p.x, at + n * E - shift + i, DT) : -INFINITY;
+        return U::make(v);
+    };
+    auto full = [&](int n) { return n * E >= shift && n * E - shift + E <= p.C; };
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int n = t + k * kStep;
+        if (n < units && full(n)) u[k] = U::load(p.x, at + (long long)n * E - shift);
+        else u[k] = U::nothing();
+    }
+    Row r = {};
     if (there) {
-        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(p.x) + row * p.ld_x * (16 / E));
+        r = row_of<DT>(p, row);
+        if (t == 0 && !full(0)) u[0] = partial(0);
+        if (units > 1 && (units - 1) % kStep == t && !full(units - 1)) {
+            const uint4 last = partial(units - 1);
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                if (t + k * kStep == units - 1) u[k] = last;
+        }
+    }
+    Part a = part_of<DT, V>(u, used);
+    if (p.smoothing != 0.0f)
 #pragma unroll
         for (int k = 0; k < V; ++k)
-            if (k < vecs - 1 || (k == vecs - 1 && count_last == E)) u[k] = __ldcs(src + t + k * G * CL);
-            else if (k == vecs - 1) {                    // the row's end inside a vector
-                float v[8] = {};
+            if (k < used)
 #pragma unroll
-                for (int i = 0; i < E; ++i) if (i < count_last) v[i] = load1(p.x, row * p.ld_x + (long long)last * E + i, DT);
-                u[k] = vec_of<DT>(v);
-            }
-        r = row_of<DT>(p, row);
-    }
-    const Part a = join_all<G, CL>(part_of<DT, V>(u, vecs, count_last), shared);
+                for (int i = 0; i < E; ++i)
+                    if ((unsigned)((t + k * kStep) * E - shift + i) < (unsigned)p.C) a.t += U::get(u[k], i);
+    a = join_all<G, CL>(a, shared);
     if (there && p.loss && t == 0) p.loss[row] = loss_of(p, r, a);
     if (there && p.dx) {
-        const float inv = 1.0f / a.s, off = p.smoothing / (float)p.C;
-        uint4* dst = reinterpret_cast<uint4*>(static_cast<char*>(p.dx) + row * p.ld_dx * (16 / E));
+        const Slope slope(p, r, a);
+        const float own = slope(r.label_x) - r.g * (1.0f - p.smoothing);         // the label's element
+        const bool labelled = !r.ignored && !r.bad;
+        const bool alike = U::shift(p.dx, to) == shift;
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (k < vecs) {
-                float v[8];
-                const long long j0 = (long long)(t + k * G * CL) * E;
+        for (int k = 0; k < V; ++k) {
+            if (k >= used) break;
+            const int n = t + k * kStep;
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] = r.ignored ? 0.0f : slope(U::get(u[k], i));
+            if (alike || G < 32) {
+                if (alike && n < units && full(n)) U::store(p.dx, to + (long long)n * E - shift, U::make(v));
+                else if (n < units)
+#pragma unroll
+                    for (int i = 0; i < E; ++i)
+                        if ((unsigned)(n * E - shift + i) < (unsigned)p.C) store1(p.dx, to + n * E - shift + i, DT, v[i]);
+            } else {
+                uint4* mine = staged + (threadIdx.x & ~31u);
+                mine[lane] = U::make(v);
+                __syncwarp();
+                const int j0 = (n - lane) * E - shift;
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    float d = __expf(elem<DT>(u[k], i) - a.m) * inv - off;
-                    if (j0 + i == r.label) d -= 1.0f - p.smoothing;
-                    v[i] = r.ignored ? 0.0f : r.bad ? NAN : d * r.g;
+                    const int j = j0 + 32 * i + lane;
+                    if ((unsigned)j >= (unsigned)p.C) continue;
+                    if (j == r.label && labelled) store1(p.dx, to + j, DT, own);
+                    else if (DT == FP_DTYPE_F32) static_cast<float*>(p.dx)[to + j] = reinterpret_cast<const float*>(mine)[32 * i + lane];
+                    else static_cast<uint16_t*>(p.dx)[to + j] = reinterpret_cast<const uint16_t*>(mine)[32 * i + lane];
                 }
-                if (k < vecs - 1 || count_last == E) __stcs(dst + t + k * G * CL, vec_of<DT>(v));
-                else
-#pragma unroll
-                    for (int i = 0; i < E; ++i) if (i < count_last) store1(p.dx, row * p.ld_dx + j0 + i, DT, v[i]);
+                __syncwarp();
             }
+        }
+        if ((alike || G < 32) && labelled && (int)((r.label + shift) / E) % kStep == t)      // the thread that has just written it
+            store1(p.dx, to + r.label, DT, own);
     }
     if (CL > 1) tc::cluster_sync_all();                  // no block leaves while another may still read its part
 }
 
-// Rows that do not fit, or do not start at 16-byte boundaries: read twice, an element at a time.
+// Rows that do not fit: read twice, an element at a time, by CL blocks.
 template <int DT, int CL>
 __global__ void __launch_bounds__(1024) cross_entropy_twice_kernel(const LossParams p) {
     __shared__ Part shared[33];
-    const long long row = (long long)(blockIdx.x / CL);
+    const long long row = (long long)(blockIdx.x / CL), step = 1024 * CL;
     const int t = (int)(blockIdx.x % CL) * 1024 + (int)threadIdx.x;
     const long long at = row * p.ld_x, to = row * p.ld_dx;
     const Row r = row_of<DT>(p, row);
     Part a = {-INFINITY, 0.0f, 0.0f};
     constexpr int U = 8;
 #pragma unroll 1
-    for (int j = t; j < p.C; j += U * 1024 * CL) {
+    for (long long j = t; j < p.C; j += U * step) {
         float x[U], m = a.m;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            x[u] = j + u * 1024 * CL < p.C ? load1(p.x, at + j + u * 1024 * CL, DT) : -INFINITY;
+            x[u] = j + u * step < p.C ? load1(p.x, at + j + u * step, DT) : -INFINITY;
             m = fmaxf(m, x[u]);
         }
         const float m0 = m == -INFINITY ? 0.0f : m;
-        if (m > a.m) a.s = a.m == -INFINITY ? 0.0f : a.s * __expf(a.m - m);
+        if (m > a.m) a.s *= exp_of(a.m - m);             // (0 from -inf)
         a.m = m;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (j + u * 1024 * CL < p.C) { a.t += x[u]; a.s += __expf(x[u] - m0); }
+        for (int u = 0; u < U; ++u) {
+            a.s += exp_of(x[u] - m0);
+            if (j + u * step < p.C) a.t += x[u];
+        }
     }
-    a = join_all<1024, CL>(a, shared);
+    a = join_all<1024, CL>(a, shared);                   // (and all have read the label's logit: dx may be x)
     if (p.loss && t == 0) p.loss[row] = loss_of(p, r, a);
     if (p.dx) {
-        const float inv = 1.0f / a.s, off = p.smoothing / (float)p.C;
-        if (CL == 1) __syncthreads();                    // the label's logit has been read by all (dx may be x); a cluster has met above
+        const Slope slope(p, r, a);
 #pragma unroll 1
-        for (int j = t; j < p.C; j += U * 1024 * CL) {
+        for (long long j = t; j < p.C; j += U * step) {
             float x[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) x[u] = j + u * 1024 * CL < p.C ? load1(p.x, at + j + u * 1024 * CL, DT) : 0.0f;
+            for (int u = 0; u < U; ++u) x[u] = j + u * step < p.C ? load1(p.x, at + j + u * step, DT) : 0.0f;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int c = j + u * 1024 * CL;
-                if (c >= p.C) break;
-                float d = __expf(x[u] - a.m) * inv - off;
-                if (c == r.label) d -= 1.0f - p.smoothing;
-                store1(p.dx, to + c, DT, r.ignored ? 0.0f : r.bad ? NAN : d * r.g);
-            }
+            for (int u = 0; u < U; ++u)
+                if (j + u * step < p.C) store1(p.dx, to + j + u * step, DT, r.ignored ? 0.0f : slope(x[u]));
         }
+        if (!r.ignored && !r.bad && r.label % step == t) store1(p.dx, to + r.label, DT, slope(r.label_x) - r.g * (1.0f - p.smoothing));
     }
     if (CL > 1) tc::cluster_sync_all();
 }
@@ -234,23 +317,21 @@ __global__ void __launch_bounds__(1024) cross_entropy_twice_kernel(const LossPar
 typedef void (*Kernel)(const LossParams);
 struct Choice { Kernel k; int threads, rows_a_block, cluster; };
 
-constexpr int kMaxVecs = 8;
-// The fewest threads that hold a row in kMaxVecs vectors each.
+// The fewest threads that hold a row; for few long rows as many blocks as that spreads it over.
 template <int DT>
-Choice choose(long long C, long long rows, bool vectors) {
+Choice choose(long long C, long long rows) {
     const int sms = sm_count();
-    const long long vecs = (C + Elems<DT>::kPer - 1) / Elems<DT>::kPer;
-    if (vectors) {
-        if (vecs <= 8 * 4) return {cross_entropy_kernel<DT, 8, 4, 1>, 256, 32, 1};
-        if (vecs <= 32 * 8) return {cross_entropy_kernel<DT, 32, 8, 1>, 256, 8, 1};
-        if (vecs <= 256 * 4) return {cross_entropy_kernel<DT, 256, 4, 1>, 256, 1, 1};
-        if (vecs <= 512 * 8) return {cross_entropy_kernel<DT, 512, 8, 1>, 512, 1, 1};
-        if (vecs <= 1024 * 8 && rows * 4 > sms) return {cross_entropy_kernel<DT, 1024, 8, 1>, 1024, 1, 1};
-        if (vecs <= 1024 * 8 * 4) return {cross_entropy_kernel<DT, 1024, 8, 4>, 1024, 1, 4};
-        if (vecs <= 1024 * 8 * 8) return {cross_entropy_kernel<DT, 1024, 8, 8>, 1024, 1, 8};
-    }
-    if (C > 16384 && rows * 8 <= 2 * sms) return {cross_entropy_twice_kernel<DT, 8>, 1024, 1, 8};
-    return {cross_entropy_twice_kernel<DT, 1>, 1024, 1, 1};
+    const long long units = (C - 1) / Unit<DT>::E + 2;   // at the worst alignment
+    if (units <= 8 * 4) return {cross_entropy_kernel<DT, 8, 4, 1>, 256, 32, 1};
+    if (units <= 32 * 4) return {cross_entropy_kernel<DT, 32, 4, 1>, 256, 8, 1};
+    if (units <= 32 * 8 && rows > 8 * sms) return {cross_entropy_kernel<DT, 32, 8, 1>, 256, 8, 1};
+    if (units <= 256 * 4) return {cross_entropy_kernel<DT, 256, 4, 1>, 256, 1, 1};
+    if (units <= 512 * 8 && rows * 8 > sms) return {cross_entropy_kernel<DT, 512, 8, 1>, 512, 1, 1};
+    if (units <= 512 * 8 * 2 && rows * 8 > sms) return {cross_entropy_kernel<DT, 512, 8, 2>, 512, 1, 2};
+    if (units <= 512 * 8 * 4 && rows * 8 > sms) return {cross_entropy_kernel<DT, 512, 8, 4>, 512, 1, 4};
+    if (units <= 512 * 4 * 8) return {cross_entropy_kernel<DT, 512, 4, 8>, 512, 1, 8};
+    if (units <= 512 * 8 * 8) return {cross_entropy_kernel<DT, 512, 8, 8>, 512, 1, 8};
+    return {cross_entropy_twice_kernel<DT, 8>, 1024, 1, 8};
 }
 
 }  // namespace
@@ -287,10 +368,8 @@ extern "C" fp_status fp_cross_entropy(const fp_cross_entropy_args* a, void* stre
     p.x = a->d_logits; p.labels = a->d_labels; p.row_grad = a->d_row_grad; p.loss = a->d_loss; p.dx = a->d_dlogits;
     p.ld_x = a->ld_logits; p.ld_dx = a->ld_dlogits; p.ignore = a->ignore_index; p.rows = a->rows; p.C = (int)a->classes; p.label_bytes = a->label_bytes;
     p.smoothing = a->label_smoothing; p.scale = a->grad_scale;
-    const bool vectors = (((uintptr_t)a->d_logits | (uintptr_t)a->d_dlogits) & 15) == 0 &&
-                         (a->rows == 1 || (a->ld_logits * bytes % 16 == 0 && (!a->d_dlogits || a->ld_dlogits * bytes % 16 == 0)));
-    const Choice c = a->dtype == FP_DTYPE_F32 ? choose<FP_DTYPE_F32>(p.C, p.rows, vectors) : a->dtype == FP_DTYPE_BF16 ? choose<FP_DTYPE_BF16>(p.C, p.rows, vectors)
-                                                                                          : choose<FP_DTYPE_F16>(p.C, p.rows, vectors);
+    const Choice c = a->dtype == FP_DTYPE_F32 ? choose<FP_DTYPE_F32>(p.C, p.rows) : a->dtype == FP_DTYPE_BF16 ? choose<FP_DTYPE_BF16>(p.C, p.rows)
+                                                                                                        : choose<FP_DTYPE_F16>(p.C, p.rows);
     const long long blocks = (a->rows + c.rows_a_block - 1) / c.rows_a_block * c.cluster;
     if (blocks > 0x7fffffffll) return err(FP_ERR_BOUNDS, "fp_cross_entropy: too many rows of this length");
     cudaLaunchConfig_t cfg;
