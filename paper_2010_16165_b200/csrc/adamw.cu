@@ -5,6 +5,7 @@
 // step over a whole network is one launch with nothing to copy beforehand and nothing to keep; a block finds its tensor
 // by bisection over the tensors' first blocks.
 #include "train_common.cuh"
+#include "tc_common.cuh"
 
 #include <math.h>
 #include <string.h>
@@ -18,8 +19,8 @@ namespace {
 using namespace train;
 
 constexpr int kThreads = 256;
-constexpr int kMaxTensors = 360;
-constexpr int kUnit32 = 4096, kUnit8 = 4096;             // elements of a block of threads
+constexpr int kMaxTensors = 320;
+constexpr int kUnit32 = 2048, kUnit8 = 4096;             // elements of a block of threads
 
 struct Entry {
     void* p;
@@ -32,10 +33,11 @@ struct Entry {
     long long n;
     long long per_row;
     int unit0;                                           // first block of threads
+    tc::FastDiv rows;                                    // division by per_row; rows.d 0: beyond 31 bits
     int aligned;                                         // whether four (32-bit states) or eight (8-bit) neighbours lie aligned everywhere
 };
 struct Step {
-    float decay, b1, ob1, b2, ob2, inv_sqrt_c2, eps, rate, grad_scale;
+    float decay, b1, ob1, b2, ob2, inv_sqrt_c2, eps, rate, grad_scale, one;
     double lr, beta1, beta2, weight_decay;
     const float* d_lr;
     const float* d_grad_scale;
@@ -69,6 +71,21 @@ __device__ __forceinline__ float updated(const Step& s, float p, float m, float 
     return __fmaf_rn(-s.rate, __fdividef(m, __fmaf_rn(r, s.inv_sqrt_c2, s.eps)), p * s.decay);
 }
 
+// Which of the elements at .. at + count - 1 (count <= 8) a mask keeps.
+__device__ __forceinline__ uint32_t kept(const Entry& e, long long at, int count) {
+    if (!e.mask) return 255u;
+    long long row = e.rows.d ? (long long)tc::fdiv((uint32_t)at, e.rows) : at / e.per_row;
+    long long left = (row + 1) * e.per_row - at;         // elements of this row from here on
+    uint32_t keep = 0, here = e.mask[row] ? 1u : 0u;
+    if (left >= count) return here ? 255u : 0u;
+    for (int i = 0; i < count; ++i) {
+        if (left == 0) { here = e.mask[++row] ? 1u : 0u; left = e.per_row; }
+        keep |= here << i;
+        --left;
+    }
+    return keep;
+}
+
 __device__ __forceinline__ const Entry& find(const Table& t, int unit) {
     int lo = 0, hi = t.count - 1;
     while (lo < hi) {
@@ -92,56 +109,128 @@ __device__ __forceinline__ Step step_of(const Table& t) {
     return s;
 }
 
+// 28 bytes an element with 32-bit parameters: 128 bytes a thread are asked for before the first is used.
 template <int PT, int GT>
 __global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant__ Table t) {
     const Entry& e = find(t, (int)blockIdx.x);
     const Step s = step_of(t);
-    const long long at0 = (long long)((int)blockIdx.x - e.unit0) * kUnit32;
+    const long long at0 = (long long)((int)blockIdx.x - e.unit0) * kUnit32 + (int)threadIdx.x * 4;
     float* m_ = static_cast<float*>(e.m);
     float* v_ = static_cast<float*>(e.v);
+    constexpr int U = kUnit32 / (4 * kThreads);
+    if (e.aligned && at0 + (U - 1) * 4 * kThreads + 4 <= e.n) {
+        float p[U][4], g[U][4], m[U][4], v[U][4];
+        uint32_t keep[U];
 #pragma unroll
-    for (int u = 0; u < kUnit32 / (4 * kThreads); ++u) {
-        const long long at = at0 + (u * kThreads + (int)threadIdx.x) * 4;
-        const int count = (int)min(4ll, e.n - at);
-        if (count <= 0) break;
-        const bool whole = e.aligned && count == 4;
-        uint32_t keep = 15;
-        if (e.mask)
-            for (int i = 0; i < count; ++i)
-                if (!e.mask[(at + i) / e.per_row]) keep &= ~(1u << i);
-        float p[4] = {0, 0, 0, 0}, g[4] = {0, 0, 0, 0}, m[4] = {0, 0, 0, 0}, v[4] = {0, 0, 0, 0};
-        if (whole) {
-            load4(e.p, at, PT, p); load4(e.g, at, GT, g); load4(m_, at, FP_DTYPE_F32, m); load4(v_, at, FP_DTYPE_F32, v);
-        } else {
-            for (int i = 0; i < count; ++i) { p[i] = load1(e.p, at + i, PT); g[i] = load1(e.g, at + i, GT); m[i] = m_[at + i]; v[i] = v_[at + i]; }
+        for (int u = 0; u < U; ++u) {
+            const long long at = at0 + u * 4 * kThreads;
+            keep[u] = kept(e, at, 4);
+            if (keep[u] & 15u) {                         // (what is pruned need not be read)
+                load4(e.p, at, PT, p[u]); load4(e.g, at, GT, g[u]); load4(m_, at, FP_DTYPE_F32, m[u]); load4(v_, at, FP_DTYPE_F32, v[u]);
+            }
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float r;
-            moments(s, g[i], m[i], v[i], r);
-            p[i] = updated(s, p[i], m[i], r);
-            if (!(keep >> i & 1)) p[i] = m[i] = v[i] = 0.0f;
+        for (int u = 0; u < U; ++u) {
+            const long long at = at0 + u * 4 * kThreads;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float r;
+                moments(s, g[u][i], m[u][i], v[u][i], r);
+                p[u][i] = updated(s, p[u][i], m[u][i], r);
+                if (!(keep[u] >> i & 1)) p[u][i] = m[u][i] = v[u][i] = 0.0f;
+            }
+            store4(e.p, at, PT, p[u]); store4(m_, at, FP_DTYPE_F32, m[u]); store4(v_, at, FP_DTYPE_F32, v[u]);
         }
-        if (whole) {
-            store4(e.p, at, PT, p); store4(m_, at, FP_DTYPE_F32, m); store4(v_, at, FP_DTYPE_F32, v);
-        } else {
-            for (int i = 0; i < count; ++i) { store1(e.p, at + i, PT, p[i]); m_[at + i] = m[i]; v_[at + i] = v[i]; }
+        return;
+    }
+#pragma unroll 1
+    for (int u = 0; u < U; ++u) {                        // a tensor's end, or one that is not aligned
+        const long long at = at0 + u * 4 * kThreads;
+        const int count = (int)max(0ll, min(4ll, e.n - at));
+        if (count == 0) break;
+        const uint32_t keep = kept(e, at, count);
+#pragma unroll 1
+        for (int i = 0; i < count; ++i) {
+            float p = load1(e.p, at + i, PT), m = m_[at + i], v = v_[at + i], r;
+            moments(s, load1(e.g, at + i, GT), m, v, r);
+            p = updated(s, p, m, r);
+            if (!(keep >> i & 1)) p = m = v = 0.0f;
+            store1(e.p, at + i, PT, p); m_[at + i] = m; v_[at + i] = v;
         }
     }
 }
 
 // ---- 8-bit states ---------------------------------------------------------------------------------------------------
-// A warp has a block of 256 elements, eight a lane; the block's largest values come from shuffles.
+// A warp has a block of 256 elements, eight a lane; the block's largest values come from shuffles.  With 16-bit parameters an element
+// is 10 bytes, for which the memory leaves 30 instructions: two elements go through one packed instruction where there is one (each half
+// rounded as by itself), and a warp asks for two blocks before it works on the first.
 
-__device__ __forceinline__ float e4m3_value(uint32_t code) {
+typedef unsigned long long Two;                          // two floats
+__device__ __forceinline__ Two two(float lo, float hi) { Two r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
+__device__ __forceinline__ Two twice(float x) { return two(x, x); }
+__device__ __forceinline__ void split(Two x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ Two mul2(Two a, Two b) { Two r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+// (A packed product and sum were contracted in spite of their .rn; as a 1 + b with a 1 that comes from the host they are not.)
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) { Two r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+__device__ __forceinline__ Two e4m3_values(uint32_t codes) {       // of the two low bytes
     uint32_t h;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)code));
-    return __half2float(__ushort_as_half((uint16_t)h));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
+    return two(__half2float(__ushort_as_half((uint16_t)h)), __half2float(__ushort_as_half((uint16_t)(h >> 16))));
 }
-__device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
+__device__ __forceinline__ uint32_t e4m3_codes(Two x) {
+    float lo, hi;
+    split(x, lo, hi);
     uint16_t r;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
+}
+__device__ __forceinline__ float quotient(float a, float b) {      // off by 2 ulp; b >= 0, and not so large that 1 / b is subnormal where a / b matters
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(b));
+    return a * r;
+}
+
+// Eight elements of a lane as they are in memory.
+template <int PT, int GT> struct Lane {
+    uint4 p[PT == FP_DTYPE_F32 ? 2 : 1], g[GT == FP_DTYPE_F32 ? 2 : 1];
+    uint2 m, v;
+    float ms, vs;
+    uint32_t keep;
+    int count;
+};
+template <int DT>
+__device__ __forceinline__ Two pair_of(const uint4* u, int i) {    // elements 2 i, 2 i + 1
+    const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, DT == FP_DTYPE_F32 ? u[DT == FP_DTYPE_F32].x : 0u, DT == FP_DTYPE_F32 ? u[DT == FP_DTYPE_F32].y : 0u,
+                           DT == FP_DTYPE_F32 ? u[DT == FP_DTYPE_F32].z : 0u, DT == FP_DTYPE_F32 ? u[DT == FP_DTYPE_F32].w : 0u};
+    if (DT == FP_DTYPE_F32) return two(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    if (DT == FP_DTYPE_BF16) return two(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+    return two(to_f32((uint16_t)w[i], DT), to_f32((uint16_t)(w[i] >> 16), DT));
+}
+template <int DT>
+__device__ __forceinline__ void read8(uint4* u, const void* x, long long at, bool whole, int count) {
+    constexpr int N = DT == FP_DTYPE_F32 ? 2 : 1, E = DT == FP_DTYPE_F32 ? 4 : 8;
+    if (whole) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) u[k] = reinterpret_cast<const uint4*>(static_cast<const char*>(x) + at * (16 / E))[k];
+        return;
+    }
+    uint32_t w[8] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < count) {
+            if (DT == FP_DTYPE_F32) w[i] = __float_as_uint(static_cast<const float*>(x)[at + i]);
+            else w[i >> 1] |= (uint32_t)static_cast<const uint16_t*>(x)[at + i] << (16 * (i & 1));
+        }
+#pragma unroll
+    for (int k = 0; k < N; ++k) u[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+}
+__device__ __forceinline__ uint2 read8_bytes(const uint8_t* x, long long at, bool whole, int count) {
+    if (whole) return *reinterpret_cast<const uint2*>(x + at);
+    uint32_t w[2] = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (i < count) w[i >> 2] |= (uint32_t)x[at + i] << (8 * (i & 3));
+    return make_uint2(w[0], w[1]);
 }
 
 template <int PT, int GT>
@@ -151,73 +240,96 @@ __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant_
     const int lane = threadIdx.x & 31;
     uint8_t* m_ = static_cast<uint8_t*>(e.m);
     uint8_t* v_ = static_cast<uint8_t*>(e.v);
-    for (int u = threadIdx.x >> 5; u < kUnit8 / FP_ADAMW_BLOCK; u += kThreads / 32) {
-        const long long block = (long long)((int)blockIdx.x - e.unit0) * (kUnit8 / FP_ADAMW_BLOCK) + u;
-        if (block * FP_ADAMW_BLOCK >= e.n) break;
-        const long long at = block * FP_ADAMW_BLOCK + lane * 8;
-        const int count = (int)max(0ll, min(8ll, e.n - at));
-        const bool whole = e.aligned && count == 8;
-        uint32_t keep = 255;
-        if (e.mask)
-            for (int i = 0; i < count; ++i)
-                if (!e.mask[(at + i) / e.per_row]) keep &= ~(1u << i);
-        float p[8], g[8];
-        uint32_t mc[8], vc[8];
-        if (whole) {
-            float a[4], b[4];
-            load4(e.p, at, PT, a); load4(e.p, at + 4, PT, b);
-            for (int i = 0; i < 4; ++i) { p[i] = a[i]; p[4 + i] = b[i]; }
-            load4(e.g, at, GT, a); load4(e.g, at + 4, GT, b);
-            for (int i = 0; i < 4; ++i) { g[i] = a[i]; g[4 + i] = b[i]; }
-            const uint2 cm = *reinterpret_cast<const uint2*>(m_ + at), cv = *reinterpret_cast<const uint2*>(v_ + at);
-            for (int i = 0; i < 4; ++i) {
-                mc[i] = cm.x >> (8 * i) & 255; mc[4 + i] = cm.y >> (8 * i) & 255;
-                vc[i] = cv.x >> (8 * i) & 255; vc[4 + i] = cv.y >> (8 * i) & 255;
-            }
-        } else {
-            for (int i = 0; i < 8; ++i) {
-                const bool in = i < count;
-                p[i] = in ? load1(e.p, at + i, PT) : 0.0f; g[i] = in ? load1(e.g, at + i, GT) : 0.0f;
-                mc[i] = in ? m_[at + i] : 0; vc[i] = in ? v_[at + i] : 0;
-            }
-        }
-        const float ms = e.m_scale[block], vs = e.v_scale[block];
-        float m[8], r[8], m_top = 0.0f, r_top = 0.0f;
+    constexpr int U = kUnit8 / FP_ADAMW_BLOCK / (kThreads / 32);
+    const long long block0 = (long long)((int)blockIdx.x - e.unit0) * (kUnit8 / FP_ADAMW_BLOCK) + (threadIdx.x >> 5);
+    Lane<PT, GT> x[U];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            m[i] = __fmul_rn(e4m3_value(mc[i]), ms);
-            r[i] = __fmul_rn(e4m3_value(vc[i]), vs);
-            float v = __fmul_rn(r[i], r[i]);
-            moments(s, g[i], m[i], v, r[i]);
-            p[i] = updated(s, p[i], m[i], r[i]);
-            if (!(keep >> i & 1) || i >= count) p[i] = m[i] = r[i] = 0.0f;
-            m_top = fmaxf(m_top, fabsf(m[i])); r_top = fmaxf(r_top, r[i]);
-        }
+    for (int u = 0; u < U; ++u) {
+        const long long block = block0 + u * (kThreads / 32), at = block * FP_ADAMW_BLOCK + lane * 8;
+        Lane<PT, GT>& y = x[u];
+        y.count = (int)max(0ll, min(8ll, e.n - at));
+        const bool whole = e.aligned && y.count == 8;
+        y.keep = y.count ? kept(e, at, y.count) : 255u;
+        read8<PT>(y.p, e.p, at, whole, y.count);
+        read8<GT>(y.g, e.g, at, whole, y.count);
+        y.m = read8_bytes(m_, at, whole, y.count);
+        y.v = read8_bytes(v_, at, whole, y.count);
+        if (block * FP_ADAMW_BLOCK < e.n) { y.ms = e.m_scale[block]; y.vs = e.v_scale[block]; }
+        else y.ms = y.vs = 0.0f;
+    }
+    const Two gs = twice(s.grad_scale), b1 = twice(s.b1), ob1 = twice(s.ob1), b2 = twice(s.b2), ob2 = twice(s.ob2), c2 = twice(s.inv_sqrt_c2),
+              eps = twice(s.eps), decay = twice(s.decay), rate = twice(-s.rate);
+    const Two one = twice(s.one);
 #pragma unroll
-        for (int d = 16; d; d >>= 1) { m_top = fmaxf(m_top, __shfl_xor_sync(~0u, m_top, d)); r_top = fmaxf(r_top, __shfl_xor_sync(~0u, r_top, d)); }
+    for (int u = 0; u < U; ++u) {
+        const long long block = block0 + u * (kThreads / 32), at = block * FP_ADAMW_BLOCK + lane * 8;
+        if (block * FP_ADAMW_BLOCK >= e.n) break;        // (the same for the whole warp)
+        const Lane<PT, GT>& y = x[u];
+        Two m[4], r[4], p[4];
+        float m_top = 0.0f, r_top = 0.0f;
+        const Two ms = twice(y.ms), vs = twice(y.vs);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            // as moments() and updated(), two at a time
+            const Two g = mul2(pair_of<GT>(y.g, i), gs);
+            m[i] = mul2(e4m3_values((i < 2 ? y.m.x : y.m.y) >> (16 * (i & 1))), ms);
+            r[i] = mul2(e4m3_values((i < 2 ? y.v.x : y.v.y) >> (16 * (i & 1))), vs);
+            m[i] = fma2(mul2(m[i], b1), one, mul2(g, ob1));
+            const Two v = fma2(mul2(mul2(r[i], r[i]), b2), one, mul2(mul2(g, ob2), g));
+            float lo, hi, a, b, c, d;
+            split(v, lo, hi);
+            lo = __fsqrt_rn(lo); hi = __fsqrt_rn(hi);
+            r[i] = two(lo, hi);
+            split(fma2(r[i], c2, eps), a, b);
+            split(m[i], c, d);
+            p[i] = fma2(rate, two(quotient(c, a), quotient(d, b)), mul2(pair_of<PT>(y.p, i), decay));
+            if (y.keep != 255u || y.count < 8) {         // pruned, or behind the tensor's end
+                const bool k0 = (y.keep >> (2 * i) & 1u) && 2 * i < y.count, k1 = (y.keep >> (2 * i + 1) & 1u) && 2 * i + 1 < y.count;
+                float q0, q1;
+                split(p[i], q0, q1);
+                p[i] = two(k0 ? q0 : 0.0f, k1 ? q1 : 0.0f);
+                c = k0 ? c : 0.0f; d = k1 ? d : 0.0f; lo = k0 ? lo : 0.0f; hi = k1 ? hi : 0.0f;
+                m[i] = two(c, d); r[i] = two(lo, hi);
+            }
+            m_top = fmaxf(m_top, fmaxf(fabsf(c), fabsf(d)));
+            r_top = fmaxf(r_top, fmaxf(lo, hi));
+        }
+        // (values that are not negative compare as their bits do)
+        m_top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(m_top)));
+        r_top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(r_top)));
         float ms1 = __fmul_rn(m_top, 1.0f / 448.0f), vs1 = __fmul_rn(r_top, 1.0f / 448.0f);
         if (ms1 < 1.17549435e-38f) ms1 = 0.0f;
         if (vs1 < 1.17549435e-38f) vs1 = 0.0f;
-        const float mi = ms1 > 0.0f ? __frcp_rn(ms1) : 0.0f, vi = vs1 > 0.0f ? __frcp_rn(vs1) : 0.0f;
+        const Two mi = twice(ms1 > 0.0f ? __frcp_rn(ms1) : 0.0f), vi = twice(vs1 > 0.0f ? __frcp_rn(vs1) : 0.0f);
+        uint32_t cm[4], cv[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            cm[i] = e4m3_codes(mul2(m[i], mi));
+            float a, b, lo, hi;
+            split(r[i], lo, hi);
+            split(mul2(r[i], vi), a, b);
+            if (lo > 0.0f) a = fmaxf(a, 0.001953125f);   // 2^-9, the smallest positive code
+            if (hi > 0.0f) b = fmaxf(b, 0.001953125f);
+            cv[i] = e4m3_codes(two(a, b));
+        }
+        const uint2 wm = make_uint2(cm[0] | cm[1] << 16, cm[2] | cm[3] << 16), wv = make_uint2(cv[0] | cv[1] << 16, cv[2] | cv[3] << 16);
         float q[8];
-        uint2 cm, cv;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = __fmul_rn(m[i], mi);
-        cm.x = e4m3_pair(q[0], q[1]) | e4m3_pair(q[2], q[3]) << 16; cm.y = e4m3_pair(q[4], q[5]) | e4m3_pair(q[6], q[7]) << 16;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { q[i] = __fmul_rn(r[i], vi); if (r[i] > 0.0f) q[i] = fmaxf(q[i], 0.001953125f); }
-        cv.x = e4m3_pair(q[0], q[1]) | e4m3_pair(q[2], q[3]) << 16; cv.y = e4m3_pair(q[4], q[5]) | e4m3_pair(q[6], q[7]) << 16;
-        if (whole) {
-            const float a[4] = {p[0], p[1], p[2], p[3]}, b[4] = {p[4], p[5], p[6], p[7]};
-            store4(e.p, at, PT, a); store4(e.p, at + 4, PT, b);
-            *reinterpret_cast<uint2*>(m_ + at) = cm;
-            *reinterpret_cast<uint2*>(v_ + at) = cv;
+        for (int i = 0; i < 4; ++i) split(p[i], q[2 * i], q[2 * i + 1]);
+        if (e.aligned && y.count == 8) {
+            const float a[4] = {q[0], q[1], q[2], q[3]}, b[4] = {q[4], q[5], q[6], q[7]};
+            if (PT == FP_DTYPE_F32) { store4(e.p, at, PT, a); store4(e.p, at + 4, PT, b); }
+            else *reinterpret_cast<uint4*>(static_cast<uint16_t*>(e.p) + at) = make_uint4(to_16x2(a[0], a[1], PT), to_16x2(a[2], a[3], PT), to_16x2(b[0], b[1], PT), to_16x2(b[2], b[3], PT));
+            *reinterpret_cast<uint2*>(m_ + at) = wm;
+            *reinterpret_cast<uint2*>(v_ + at) = wv;
         } else {
-            for (int i = 0; i < count; ++i) {
-                store1(e.p, at + i, PT, p[i]);
-                m_[at + i] = (uint8_t)((i < 4 ? cm.x : cm.y) >> (8 * (i & 3)));
-                v_[at + i] = (uint8_t)((i < 4 ? cv.x : cv.y) >> (8 * (i & 3)));
-            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < y.count) {
+                    store1(e.p, at + i, PT, q[i]);
+                    m_[at + i] = (uint8_t)((i < 4 ? wm.x : wm.y) >> (8 * (i & 3)));
+                    v_[at + i] = (uint8_t)((i < 4 ? wv.x : wv.y) >> (8 * (i & 3)));
+                }
         }
         if (lane == 0) { e.m_scale[block] = ms1; e.v_scale[block] = vs1; }
     }
@@ -296,7 +408,7 @@ extern "C" fp_status fp_adamw_step(const fp_adamw_tensor* ts, int32_t count, con
     s.lr = h->lr; s.beta1 = h->beta1; s.beta2 = h->beta2; s.weight_decay = h->weight_decay; s.step = h->step;
     s.d_lr = h->d_lr; s.d_grad_scale = h->d_grad_scale; s.d_step = reinterpret_cast<const int64_t*>(h->d_step);
     s.b1 = (float)h->beta1; s.ob1 = (float)(1.0 - h->beta1); s.b2 = (float)h->beta2; s.ob2 = (float)(1.0 - h->beta2);
-    s.eps = (float)h->eps; s.grad_scale = (float)h->grad_scale;
+    s.eps = (float)h->eps; s.grad_scale = (float)h->grad_scale; s.one = 1.0f;
     scalars(s, h->lr, h->d_step ? 1 : h->step);
     t.count = 0;
     static const int kinds[3] = {FP_DTYPE_F32, FP_DTYPE_BF16, FP_DTYPE_F16};
@@ -318,6 +430,8 @@ extern "C" fp_status fp_adamw_step(const fp_adamw_tensor* ts, int32_t count, con
                     Entry& r = t.e[t.count++];
                     r.p = x.d_p; r.g = x.d_g; r.m = x.d_m; r.v = x.d_v; r.m_scale = x.d_m_scale; r.v_scale = x.d_v_scale;
                     r.mask = x.d_mask; r.n = x.n; r.per_row = x.per_row; r.unit0 = (int)units;
+                    memset(&r.rows, 0, sizeof(r.rows));
+                    if (x.d_mask && x.n < (1ll << 31) && x.per_row < (1ll << 31)) r.rows = tc::make_fastdiv((uint32_t)x.per_row);
                     const int vec = bits == 32 ? 4 : 8;
                     r.aligned = multiple(x.d_p, std::min(16, vec * elem_bytes(pt))) && multiple(x.d_g, std::min(16, vec * elem_bytes(gt))) &&
                                 multiple(x.d_m, bits == 32 ? 16 : 8) && multiple(x.d_v, bits == 32 ? 16 : 8);
