@@ -460,8 +460,8 @@ typedef struct {
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
  * in 32 bits, p rounded once to its type.  8-bit states are kept in blocks of 256 elements of a tensor: code =
  * e4m3(x / scale), scale = largest |x| of the block / 448, rounded to nearest even; of v the square root is kept, which halves
- * its exponent range, and a positive one never becomes 0 (it takes the smallest code), so that no
- * step is divided by eps alone because of rounding.  The step itself uses m and v before they are rounded.
+ * its exponent range (taken to 2^-22 of itself; v below 2^-126 counts as 0), and a positive one never becomes 0 (it takes the smallest code),
+ * so that no step is divided by eps alone because of rounding.  The step itself uses m and v before they are rounded.
  *   h_tensors   host; read before the call returns.  No two tensors may overlap.
  * Errors: FP_ERR_ARG, FP_ERR_UNSUPPORTED (dtype, state_bits), FP_ERR_BOUNDS (n beyond 2^40), FP_ERR_CUDA; they are found
  * before anything is launched, except FP_ERR_CUDA.

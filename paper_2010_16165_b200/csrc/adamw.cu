@@ -34,7 +34,7 @@ struct Entry {
     long long per_row;
     int unit0;                                           // first block of threads
     tc::FastDiv rows;                                    // division by per_row; rows.d 0: beyond 31 bits
-    int aligned;                                         // whether four (32-bit states) or eight (8-bit) neighbours lie aligned everywhere
+    int aligned;                                         // whether four (32-bit states) or sixteen (8-bit) neighbours lie in aligned vectors everywhere
 };
 struct Step {
     float decay, b1, ob1, b2, ob2, inv_sqrt_c2, eps, rate, grad_scale, one;
@@ -71,18 +71,21 @@ __device__ __forceinline__ float updated(const Step& s, float p, float m, float 
     return __fmaf_rn(-s.rate, __fdividef(m, __fmaf_rn(r, s.inv_sqrt_c2, s.eps)), p * s.decay);
 }
 
-// Which of the elements at .. at + count - 1 (count <= 8) a mask keeps.
+// Which of the elements at .. at + count - 1 (count <= 16) a mask keeps.
 __device__ __forceinline__ uint32_t kept(const Entry& e, long long at, int count) {
-    if (!e.mask) return 255u;
+    if (!e.mask) return 0xffffu;
     long long row = e.rows.d ? (long long)tc::fdiv((uint32_t)at, e.rows) : at / e.per_row;
-    long long left = (row + 1) * e.per_row - at;         // elements of this row from here on
-    uint32_t keep = 0, here = e.mask[row] ? 1u : 0u;
-    if (left >= count) return here ? 255u : 0u;
-    for (int i = 0; i < count; ++i) {
-        if (left == 0) { here = e.mask[++row] ? 1u : 0u; left = e.per_row; }
-        keep |= here << i;
-        --left;
-    }
+    const long long left = (row + 1) * e.per_row - at;   // elements of this row from here on
+    uint32_t keep = e.mask[row] ? 0xffffu : 0u;
+    if (left >= count) return keep;
+    int from = (int)left;                                // where the next row begins
+    keep &= (1u << from) - 1u;
+#pragma unroll 1
+    do {
+        const uint32_t rest = 0xffffu << from;
+        from += (int)min(16ll, e.per_row);
+        keep = (keep & ~rest) | (e.mask[++row] ? rest & 0xffffu : 0u);
+    } while (from < count);
     return keep;
 }
 
@@ -161,9 +164,10 @@ __global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant
 }
 
 // ---- 8-bit states ---------------------------------------------------------------------------------------------------
-// A warp has a block of 256 elements, eight a lane; the block's largest values come from shuffles.  With 16-bit parameters an element
-// is 10 bytes, for which the memory leaves 30 instructions: two elements go through one packed instruction where there is one (each half
-// rounded as by itself), and a warp asks for two blocks before it works on the first.
+// Half a warp has a block of 256 elements, sixteen a lane; the block's largest values come from shuffles.  With 16-bit parameters an
+// element is 10 bytes, for which the memory leaves 27 instructions, hence: two elements go through one packed instruction where there
+// is one (each half rounded as by itself), what a block needs once is paid for by sixteen elements, and the root is the approximate
+// one, off by 2^-22 of itself at most: with the exact one 315 M elements took 368 us instead of 318.
 
 typedef unsigned long long Two;                          // two floats
 __device__ __forceinline__ Two two(float lo, float hi) { Two r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
@@ -191,148 +195,150 @@ __device__ __forceinline__ float quotient(float a, float b) {      // off by 2 u
     return a * r;
 }
 
-// Eight elements of a lane as they are in memory.
-template <int PT, int GT> struct Lane {
-    uint4 p[PT == FP_DTYPE_F32 ? 2 : 1], g[GT == FP_DTYPE_F32 ? 2 : 1];
-    uint2 m, v;
-    float ms, vs;
-    uint32_t keep;
-    int count;
-};
-template <int DT>
-__device__ __forceinline__ Two pair_of(const uint4* u, int i) {    // elements 2 i, 2 i + 1
-    const uint32_t w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, DT == FP_DTYPE_F32 ? u[DT == FP_DTYPE_F32].x : 0u, DT == FP_DTYPE_F32 ? u[DT == FP_DTYPE_F32].y : 0u,
-                           DT == FP_DTYPE_F32 ? u[DT == FP_DTYPE_F32].z : 0u, DT == FP_DTYPE_F32 ? u[DT == FP_DTYPE_F32].w : 0u};
-    if (DT == FP_DTYPE_F32) return two(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
-    if (DT == FP_DTYPE_BF16) return two(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
-    return two(to_f32((uint16_t)w[i], DT), to_f32((uint16_t)(w[i] >> 16), DT));
+__device__ __forceinline__ float root(float x) {                    // below 2^-126: 0
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
 }
-template <int DT>
-__device__ __forceinline__ void read8(uint4* u, const void* x, long long at, bool whole, int count) {
-    constexpr int N = DT == FP_DTYPE_F32 ? 2 : 1, E = DT == FP_DTYPE_F32 ? 4 : 8;
-    if (whole) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) u[k] = reinterpret_cast<const uint4*>(static_cast<const char*>(x) + at * (16 / E))[k];
-        return;
+
+// Sixteen elements of a type as they are in memory.
+template <int DT> struct Sixteen {
+    uint32_t w[DT == FP_DTYPE_F32 ? 16 : 8];
+    __device__ __forceinline__ Two pair(int i) const {             // elements 2 i, 2 i + 1
+        if (DT == FP_DTYPE_F32) return two(__uint_as_float(w[(2 * i) % (DT == FP_DTYPE_F32 ? 16 : 8)]), __uint_as_float(w[(2 * i + 1) % (DT == FP_DTYPE_F32 ? 16 : 8)]));
+        if (DT == FP_DTYPE_BF16) return two(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+        return two(to_f32((uint16_t)w[i], DT), to_f32((uint16_t)(w[i] >> 16), DT));
     }
-    uint32_t w[8] = {};
+    __device__ __forceinline__ void put(int i, float lo, float hi) {
+        if (DT == FP_DTYPE_F32) { w[(2 * i) % (DT == FP_DTYPE_F32 ? 16 : 8)] = __float_as_uint(lo); w[(2 * i + 1) % (DT == FP_DTYPE_F32 ? 16 : 8)] = __float_as_uint(hi); }
+        else w[i] = to_16x2(lo, hi, DT);
+    }
+    static constexpr int kBytes = DT == FP_DTYPE_F32 ? 4 : 2;      // of an element, and so vectors of sixteen elements
+    __device__ __forceinline__ void read(const void* x, long long at) {
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const char*>(x) + at * kBytes);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < count) {
-            if (DT == FP_DTYPE_F32) w[i] = __float_as_uint(static_cast<const float*>(x)[at + i]);
-            else w[i >> 1] |= (uint32_t)static_cast<const uint16_t*>(x)[at + i] << (16 * (i & 1));
+        for (int k = 0; k < kBytes; ++k) { const uint4 u = src[k]; w[4 * k] = u.x; w[4 * k + 1] = u.y; w[4 * k + 2] = u.z; w[4 * k + 3] = u.w; }
+    }
+    __device__ __forceinline__ void write(void* x, long long at) const {
+        uint4* dst = reinterpret_cast<uint4*>(static_cast<char*>(x) + at * kBytes);
+#pragma unroll
+        for (int k = 0; k < kBytes; ++k) dst[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+    }
+    __device__ __forceinline__ void read(const void* x, long long at, int count) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) put(i, 2 * i < count ? load1(x, at + 2 * i, DT) : 0.0f, 2 * i + 1 < count ? load1(x, at + 2 * i + 1, DT) : 0.0f);
+    }
+    __device__ __forceinline__ void write(void* x, long long at, int count) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float lo, hi;
+            split(pair(i), lo, hi);
+            if (2 * i < count) store1(x, at + 2 * i, DT, lo);
+            if (2 * i + 1 < count) store1(x, at + 2 * i + 1, DT, hi);
         }
+    }
+};
+
+__device__ __forceinline__ uint4 read_codes(const uint8_t* x, long long at, int count) {
+    uint32_t w[4] = {};
 #pragma unroll
-    for (int k = 0; k < N; ++k) u[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+    for (int i = 0; i < 16; ++i) if (i < count) w[i >> 2] |= (uint32_t)x[at + i] << (8 * (i & 3));
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ uint2 read8_bytes(const uint8_t* x, long long at, bool whole, int count) {
-    if (whole) return *reinterpret_cast<const uint2*>(x + at);
-    uint32_t w[2] = {};
+__device__ __forceinline__ void write_codes(uint8_t* x, long long at, int count, const uint32_t (&w)[4]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) if (i < count) w[i >> 2] |= (uint32_t)x[at + i] << (8 * (i & 3));
-    return make_uint2(w[0], w[1]);
+    for (int i = 0; i < 16; ++i) if (i < count) x[at + i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+}
+
+// The largest of the values of half a warp, none of them negative (so they compare as their bits do).
+__device__ __forceinline__ float largest_of_half(float x) {
+#pragma unroll
+    for (int d = 8; d; d >>= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
+    return x;
 }
 
 template <int PT, int GT>
 __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant__ Table t) {
     const Entry& e = find(t, (int)blockIdx.x);
     const Step s = step_of(t);
-    const int lane = threadIdx.x & 31;
+    const int lane16 = threadIdx.x & 15;
     uint8_t* m_ = static_cast<uint8_t*>(e.m);
     uint8_t* v_ = static_cast<uint8_t*>(e.v);
-    constexpr int U = kUnit8 / FP_ADAMW_BLOCK / (kThreads / 32);
-    const long long block0 = (long long)((int)blockIdx.x - e.unit0) * (kUnit8 / FP_ADAMW_BLOCK) + (threadIdx.x >> 5);
-    Lane<PT, GT> x[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const long long block = block0 + u * (kThreads / 32), at = block * FP_ADAMW_BLOCK + lane * 8;
-        Lane<PT, GT>& y = x[u];
-        y.count = (int)max(0ll, min(8ll, e.n - at));
-        const bool whole = e.aligned && y.count == 8;
-        y.keep = y.count ? kept(e, at, y.count) : 255u;
-        read8<PT>(y.p, e.p, at, whole, y.count);
-        read8<GT>(y.g, e.g, at, whole, y.count);
-        y.m = read8_bytes(m_, at, whole, y.count);
-        y.v = read8_bytes(v_, at, whole, y.count);
-        if (block * FP_ADAMW_BLOCK < e.n) { y.ms = e.m_scale[block]; y.vs = e.v_scale[block]; }
-        else y.ms = y.vs = 0.0f;
+    static_assert(kUnit8 == 16 * kThreads && FP_ADAMW_BLOCK == 256, "half a warp a block");
+    const long long block = (long long)((int)blockIdx.x - e.unit0) * (kUnit8 / FP_ADAMW_BLOCK) + (threadIdx.x >> 4), at = block * FP_ADAMW_BLOCK + lane16 * 16;
+    const int count = (int)max(0ll, min(16ll, e.n - at));
+    const bool whole = e.aligned && count == 16;
+    Sixteen<PT> p;
+    Sixteen<GT> g;
+    uint4 mc, vc;
+    if (whole) {
+        p.read(e.p, at); g.read(e.g, at);
+        mc = *reinterpret_cast<const uint4*>(m_ + at); vc = *reinterpret_cast<const uint4*>(v_ + at);
+    } else {
+        p.read(e.p, at, count); g.read(e.g, at, count);
+        mc = read_codes(m_, at, count); vc = read_codes(v_, at, count);
     }
+    const bool there = block * FP_ADAMW_BLOCK < e.n;
+    const float ms0 = there ? e.m_scale[block] : 0.0f, vs0 = there ? e.v_scale[block] : 0.0f;
+    const uint32_t keep = count ? kept(e, at, count) & ((1u << count) - 1u) : 0u;
     const Two gs = twice(s.grad_scale), b1 = twice(s.b1), ob1 = twice(s.ob1), b2 = twice(s.b2), ob2 = twice(s.ob2), c2 = twice(s.inv_sqrt_c2),
-              eps = twice(s.eps), decay = twice(s.decay), rate = twice(-s.rate);
-    const Two one = twice(s.one);
+              eps = twice(s.eps), decay = twice(s.decay), rate = twice(-s.rate), one = twice(s.one), ms = twice(ms0), vs = twice(vs0);
+    const uint32_t mw[4] = {mc.x, mc.y, mc.z, mc.w}, vw[4] = {vc.x, vc.y, vc.z, vc.w};
+    Two m[8], r[8];
+    float m_top = 0.0f, r_top = 0.0f;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const long long block = block0 + u * (kThreads / 32), at = block * FP_ADAMW_BLOCK + lane * 8;
-        if (block * FP_ADAMW_BLOCK >= e.n) break;        // (the same for the whole warp)
-        const Lane<PT, GT>& y = x[u];
-        Two m[4], r[4], p[4];
-        float m_top = 0.0f, r_top = 0.0f;
-        const Two ms = twice(y.ms), vs = twice(y.vs);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            // as moments() and updated(), two at a time
-            const Two g = mul2(pair_of<GT>(y.g, i), gs);
-            m[i] = mul2(e4m3_values((i < 2 ? y.m.x : y.m.y) >> (16 * (i & 1))), ms);
-            r[i] = mul2(e4m3_values((i < 2 ? y.v.x : y.v.y) >> (16 * (i & 1))), vs);
-            m[i] = fma2(mul2(m[i], b1), one, mul2(g, ob1));
-            const Two v = fma2(mul2(mul2(r[i], r[i]), b2), one, mul2(mul2(g, ob2), g));
-            float lo, hi, a, b, c, d;
-            split(v, lo, hi);
-            lo = __fsqrt_rn(lo); hi = __fsqrt_rn(hi);
-            r[i] = two(lo, hi);
-            split(fma2(r[i], c2, eps), a, b);
-            split(m[i], c, d);
-            p[i] = fma2(rate, two(quotient(c, a), quotient(d, b)), mul2(pair_of<PT>(y.p, i), decay));
-            if (y.keep != 255u || y.count < 8) {         // pruned, or behind the tensor's end
-                const bool k0 = (y.keep >> (2 * i) & 1u) && 2 * i < y.count, k1 = (y.keep >> (2 * i + 1) & 1u) && 2 * i + 1 < y.count;
-                float q0, q1;
-                split(p[i], q0, q1);
-                p[i] = two(k0 ? q0 : 0.0f, k1 ? q1 : 0.0f);
-                c = k0 ? c : 0.0f; d = k1 ? d : 0.0f; lo = k0 ? lo : 0.0f; hi = k1 ? hi : 0.0f;
-                m[i] = two(c, d); r[i] = two(lo, hi);
-            }
-            m_top = fmaxf(m_top, fmaxf(fabsf(c), fabsf(d)));
-            r_top = fmaxf(r_top, fmaxf(lo, hi));
+    for (int i = 0; i < 8; ++i) {
+        // as moments() and updated(), two at a time
+        const Two d = mul2(g.pair(i), gs);
+        m[i] = mul2(e4m3_values(mw[i >> 1] >> (16 * (i & 1))), ms);
+        r[i] = mul2(e4m3_values(vw[i >> 1] >> (16 * (i & 1))), vs);
+        m[i] = fma2(mul2(m[i], b1), one, mul2(d, ob1));
+        const Two v = fma2(mul2(mul2(r[i], r[i]), b2), one, mul2(mul2(d, ob2), d));
+        float lo, hi, a, b, x, y, q0, q1;
+        split(v, lo, hi);
+        lo = root(lo); hi = root(hi);
+        r[i] = two(lo, hi);
+        split(fma2(r[i], c2, eps), a, b);
+        split(m[i], x, y);
+        split(fma2(rate, two(quotient(x, a), quotient(y, b)), mul2(p.pair(i), decay)), q0, q1);
+        if (keep != 0xffffu) {                           // pruned, or behind the tensor's end
+            const bool k0 = keep >> (2 * i) & 1u, k1 = keep >> (2 * i + 1) & 1u;
+            q0 = k0 ? q0 : 0.0f; q1 = k1 ? q1 : 0.0f; x = k0 ? x : 0.0f; y = k1 ? y : 0.0f; lo = k0 ? lo : 0.0f; hi = k1 ? hi : 0.0f;
+            m[i] = two(x, y); r[i] = two(lo, hi);
         }
-        // (values that are not negative compare as their bits do)
-        m_top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(m_top)));
-        r_top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(r_top)));
-        float ms1 = __fmul_rn(m_top, 1.0f / 448.0f), vs1 = __fmul_rn(r_top, 1.0f / 448.0f);
-        if (ms1 < 1.17549435e-38f) ms1 = 0.0f;
-        if (vs1 < 1.17549435e-38f) vs1 = 0.0f;
-        const Two mi = twice(ms1 > 0.0f ? __frcp_rn(ms1) : 0.0f), vi = twice(vs1 > 0.0f ? __frcp_rn(vs1) : 0.0f);
-        uint32_t cm[4], cv[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            cm[i] = e4m3_codes(mul2(m[i], mi));
-            float a, b, lo, hi;
-            split(r[i], lo, hi);
-            split(mul2(r[i], vi), a, b);
-            if (lo > 0.0f) a = fmaxf(a, 0.001953125f);   // 2^-9, the smallest positive code
-            if (hi > 0.0f) b = fmaxf(b, 0.001953125f);
-            cv[i] = e4m3_codes(two(a, b));
-        }
-        const uint2 wm = make_uint2(cm[0] | cm[1] << 16, cm[2] | cm[3] << 16), wv = make_uint2(cv[0] | cv[1] << 16, cv[2] | cv[3] << 16);
-        float q[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) split(p[i], q[2 * i], q[2 * i + 1]);
-        if (e.aligned && y.count == 8) {
-            const float a[4] = {q[0], q[1], q[2], q[3]}, b[4] = {q[4], q[5], q[6], q[7]};
-            if (PT == FP_DTYPE_F32) { store4(e.p, at, PT, a); store4(e.p, at + 4, PT, b); }
-            else *reinterpret_cast<uint4*>(static_cast<uint16_t*>(e.p) + at) = make_uint4(to_16x2(a[0], a[1], PT), to_16x2(a[2], a[3], PT), to_16x2(b[0], b[1], PT), to_16x2(b[2], b[3], PT));
-            *reinterpret_cast<uint2*>(m_ + at) = wm;
-            *reinterpret_cast<uint2*>(v_ + at) = wv;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < y.count) {
-                    store1(e.p, at + i, PT, q[i]);
-                    m_[at + i] = (uint8_t)((i < 4 ? wm.x : wm.y) >> (8 * (i & 3)));
-                    v_[at + i] = (uint8_t)((i < 4 ? wv.x : wv.y) >> (8 * (i & 3)));
-                }
-        }
-        if (lane == 0) { e.m_scale[block] = ms1; e.v_scale[block] = vs1; }
+        p.put(i, q0, q1);
+        m_top = fmaxf(m_top, fmaxf(fabsf(x), fabsf(y)));
+        r_top = fmaxf(r_top, fmaxf(lo, hi));
     }
+    m_top = largest_of_half(m_top);
+    r_top = largest_of_half(r_top);
+    float ms1 = __fmul_rn(m_top, 1.0f / 448.0f), vs1 = __fmul_rn(r_top, 1.0f / 448.0f);
+    if (ms1 < 1.17549435e-38f) ms1 = 0.0f;
+    if (vs1 < 1.17549435e-38f) vs1 = 0.0f;
+    const Two mi = twice(ms1 > 0.0f ? __frcp_rn(ms1) : 0.0f), vi = twice(vs1 > 0.0f ? __frcp_rn(vs1) : 0.0f);
+    uint32_t cm[4], cv[4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t a = e4m3_codes(mul2(m[i], mi));
+        float lo, hi, x, y;
+        split(r[i], lo, hi);
+        split(mul2(r[i], vi), x, y);
+        if (lo > 0.0f) x = fmaxf(x, 0.001953125f);       // 2^-9, the smallest positive code
+        if (hi > 0.0f) y = fmaxf(y, 0.001953125f);
+        const uint32_t b = e4m3_codes(two(x, y));
+        cm[i >> 1] = i & 1 ? cm[i >> 1] | a << 16 : a;
+        cv[i >> 1] = i & 1 ? cv[i >> 1] | b << 16 : b;
+    }
+    if (whole) {
+        p.write(e.p, at);
+        *reinterpret_cast<uint4*>(m_ + at) = make_uint4(cm[0], cm[1], cm[2], cm[3]);
+        *reinterpret_cast<uint4*>(v_ + at) = make_uint4(cv[0], cv[1], cv[2], cv[3]);
+    } else {
+        p.write(e.p, at, count);
+        write_codes(m_, at, count, cm);
+        write_codes(v_, at, count, cv);
+    }
+    if (lane16 == 0 && there) { e.m_scale[block] = ms1; e.v_scale[block] = vs1; }
 }
 
 typedef void (*Kernel)(const Table);
@@ -432,9 +438,9 @@ extern "C" fp_status fp_adamw_step(const fp_adamw_tensor* ts, int32_t count, con
                     r.mask = x.d_mask; r.n = x.n; r.per_row = x.per_row; r.unit0 = (int)units;
                     memset(&r.rows, 0, sizeof(r.rows));
                     if (x.d_mask && x.n < (1ll << 31) && x.per_row < (1ll << 31)) r.rows = tc::make_fastdiv((uint32_t)x.per_row);
-                    const int vec = bits == 32 ? 4 : 8;
+                    const int vec = bits == 32 ? 4 : 16;
                     r.aligned = multiple(x.d_p, std::min(16, vec * elem_bytes(pt))) && multiple(x.d_g, std::min(16, vec * elem_bytes(gt))) &&
-                                multiple(x.d_m, bits == 32 ? 16 : 8) && multiple(x.d_v, bits == 32 ? 16 : 8);
+                                multiple(x.d_m, 16) && multiple(x.d_v, 16);
                     units += mine;
                 }
                 if ((e = flush(t, (unsigned)units, k, (cudaStream_t)stream)) != cudaSuccess) goto done;
