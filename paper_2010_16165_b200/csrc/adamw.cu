@@ -19,7 +19,7 @@ namespace {
 using namespace train;
 
 constexpr int kThreads = 256;
-constexpr int kMaxTensors = 320;
+constexpr int kFewTensors = 64, kMaxTensors = 320;     // of a launch: its parameters are 6 or 31 KB, copied at every call (4 us for the larger)
 constexpr int kUnit32 = 2048, kUnit8 = 4096;             // elements of a block of threads
 
 struct Entry {
@@ -44,12 +44,12 @@ struct Step {
     const int64_t* d_step;
     long long step;
 };
-struct Table {
+template <int N> struct Table {
     Step s;
     int count;
-    Entry e[kMaxTensors];
+    Entry e[N];
 };
-static_assert(sizeof(Table) <= 32764, "the launch's parameters");
+static_assert(sizeof(Table<kMaxTensors>) <= 32764, "the launch's parameters");
 
 // The step's scalars, from 64-bit arithmetic as the host does it.
 __host__ __device__ inline void scalars(Step& s, double lr, long long t) {
@@ -89,7 +89,8 @@ __device__ __forceinline__ uint32_t kept(const Entry& e, long long at, int count
     return keep;
 }
 
-__device__ __forceinline__ const Entry& find(const Table& t, int unit) {
+template <int N>
+__device__ __forceinline__ const Entry& find(const Table<N>& t, int unit) {
     int lo = 0, hi = t.count - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -98,9 +99,9 @@ __device__ __forceinline__ const Entry& find(const Table& t, int unit) {
     return t.e[lo];
 }
 
-__device__ __forceinline__ Step step_of(const Table& t) {
-    Step s = t.s;
-    if (t.s.d_lr || t.s.d_step || t.s.d_grad_scale) {
+__device__ __forceinline__ Step step_of(const Step& from) {
+    Step s = from;
+    if (s.d_lr || s.d_step || s.d_grad_scale) {
         __shared__ float got[4];
         if (threadIdx.x == 0) {
             if (s.d_lr || s.d_step) scalars(s, s.d_lr ? (double)*s.d_lr : s.lr, s.d_step ? (long long)*s.d_step : s.step);
@@ -113,10 +114,10 @@ __device__ __forceinline__ Step step_of(const Table& t) {
 }
 
 // 28 bytes an element with 32-bit parameters: 128 bytes a thread are asked for before the first is used.
-template <int PT, int GT>
-__global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant__ Table t) {
+template <int PT, int GT, int N>
+__global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant__ Table<N> t) {
     const Entry& e = find(t, (int)blockIdx.x);
-    const Step s = step_of(t);
+    const Step s = step_of(t.s);
     const long long at0 = (long long)((int)blockIdx.x - e.unit0) * kUnit32 + (int)threadIdx.x * 4;
     float* m_ = static_cast<float*>(e.m);
     float* v_ = static_cast<float*>(e.v);
@@ -257,10 +258,10 @@ __device__ __forceinline__ float largest_of_half(float x) {
     return x;
 }
 
-template <int PT, int GT>
-__global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant__ Table t) {
+template <int PT, int GT, int N>
+__global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant__ Table<N> t) {
     const Entry& e = find(t, (int)blockIdx.x);
-    const Step s = step_of(t);
+    const Step s = step_of(t.s);
     const int lane16 = threadIdx.x & 15;
     uint8_t* m_ = static_cast<uint8_t*>(e.m);
     uint8_t* v_ = static_cast<uint8_t*>(e.v);
@@ -341,31 +342,60 @@ __global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant_
     if (lane16 == 0 && there) { e.m_scale[block] = ms1; e.v_scale[block] = vs1; }
 }
 
-typedef void (*Kernel)(const Table);
-template <int PT>
-Kernel kernel_for(int gt, int bits) {
-    if (gt == FP_DTYPE_F32) return bits == 8 ? adamw8_kernel<PT, FP_DTYPE_F32> : adamw32_kernel<PT, FP_DTYPE_F32>;
-    if (gt == FP_DTYPE_BF16) return bits == 8 ? adamw8_kernel<PT, FP_DTYPE_BF16> : adamw32_kernel<PT, FP_DTYPE_BF16>;
-    return bits == 8 ? adamw8_kernel<PT, FP_DTYPE_F16> : adamw32_kernel<PT, FP_DTYPE_F16>;
+template <int PT, int GT, int N>
+const void* kernel_for(int bits) { return bits == 8 ? (const void*)adamw8_kernel<PT, GT, N> : (const void*)adamw32_kernel<PT, GT, N>; }
+template <int PT, int N>
+const void* kernel_for(int gt, int bits) {
+    return gt == FP_DTYPE_F32 ? kernel_for<PT, FP_DTYPE_F32, N>(bits) : gt == FP_DTYPE_BF16 ? kernel_for<PT, FP_DTYPE_BF16, N>(bits)
+                                                                                        : kernel_for<PT, FP_DTYPE_F16, N>(bits);
 }
-Kernel kernel_of(int pt, int gt, int bits) {
-    return pt == FP_DTYPE_F32 ? kernel_for<FP_DTYPE_F32>(gt, bits) : pt == FP_DTYPE_BF16 ? kernel_for<FP_DTYPE_BF16>(gt, bits)
-                                                                                        : kernel_for<FP_DTYPE_F16>(gt, bits);
+template <int N>
+const void* kernel_of(int pt, int gt, int bits) {
+    return pt == FP_DTYPE_F32 ? kernel_for<FP_DTYPE_F32, N>(gt, bits) : pt == FP_DTYPE_BF16 ? kernel_for<FP_DTYPE_BF16, N>(gt, bits)
+                                                                                        : kernel_for<FP_DTYPE_F16, N>(gt, bits);
 }
 bool dtype_ok(int d) { return d == FP_DTYPE_F32 || is_half(d); }
 bool multiple(const void* p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 
-cudaError_t flush(Table& t, unsigned units, Kernel k, cudaStream_t st) {
-    if (!t.count) return cudaSuccess;
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3(units);
-    cfg.blockDim = dim3(kThreads);
-    cfg.stream = st;
-    void* args[1] = {&t};
-    const cudaError_t e = cudaLaunchKernelExC(&cfg, (const void*)k, args);
+struct Kind { int p, g, bits; };
+inline bool is_of(const fp_adamw_tensor& x, const Kind& k) { return x.n > 0 && x.p_dtype == k.p && x.g_dtype == k.g && x.state_bits == k.bits; }
+
+// The tensors of one kind among ts[0 .. count), in launches of up to N.
+template <int N>
+cudaError_t run_kind(const Step& s, const fp_adamw_tensor* ts, int count, const Kind& k, cudaStream_t st) {
+    Table<N> t;                                          // at most 31 KB of stack
+    t.s = s;
     t.count = 0;
-    return e;
+    const long long unit = k.bits == 32 ? kUnit32 : kUnit8;
+    long long units = 0;
+    for (int i = 0; i <= count; ++i) {
+        if (i < count && !is_of(ts[i], k)) continue;
+        const long long mine = i < count ? (ts[i].n + unit - 1) / unit : 0;
+        if (t.count && (i == count || t.count == N || units + mine > 0x7fffffffll)) {
+            cudaLaunchConfig_t cfg;
+            memset(&cfg, 0, sizeof(cfg));
+            cfg.gridDim = dim3((unsigned)units);
+            cfg.blockDim = dim3(kThreads);
+            cfg.stream = st;
+            void* args[1] = {&t};
+            const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel_of<N>(k.p, k.g, k.bits), args);
+            if (e != cudaSuccess) return e;
+            t.count = 0;
+            units = 0;
+        }
+        if (i == count) break;
+        const fp_adamw_tensor& x = ts[i];
+        Entry& r = t.e[t.count++];
+        r.p = x.d_p; r.g = x.d_g; r.m = x.d_m; r.v = x.d_v; r.m_scale = x.d_m_scale; r.v_scale = x.d_v_scale;
+        r.mask = x.d_mask; r.n = x.n; r.per_row = x.per_row; r.unit0 = (int)units;
+        memset(&r.rows, 0, sizeof(r.rows));
+        if (x.d_mask && x.n < (1ll << 31) && x.per_row < (1ll << 31)) r.rows = tc::make_fastdiv((uint32_t)x.per_row);
+        const int vec = k.bits == 32 ? 4 : 16;
+        r.aligned = multiple(x.d_p, std::min(16, vec * elem_bytes(k.p))) && multiple(x.d_g, std::min(16, vec * elem_bytes(k.g))) &&
+                    multiple(x.d_m, 16) && multiple(x.d_v, 16);
+        units += mine;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace
@@ -408,44 +438,27 @@ extern "C" fp_status fp_adamw_step(const fp_adamw_tensor* ts, int32_t count, con
     }
     if (!there) return err(FP_ERR_ARG, "fp_adamw_step: a buffer is not memory of the current device");
 
-    Table t;                                             // 32 KB of stack
-    Step& s = t.s;
+    Step s;
     memset(&s, 0, sizeof(s));
     s.lr = h->lr; s.beta1 = h->beta1; s.beta2 = h->beta2; s.weight_decay = h->weight_decay; s.step = h->step;
     s.d_lr = h->d_lr; s.d_grad_scale = h->d_grad_scale; s.d_step = reinterpret_cast<const int64_t*>(h->d_step);
     s.b1 = (float)h->beta1; s.ob1 = (float)(1.0 - h->beta1); s.b2 = (float)h->beta2; s.ob2 = (float)(1.0 - h->beta2);
     s.eps = (float)h->eps; s.grad_scale = (float)h->grad_scale; s.one = 1.0f;
     scalars(s, h->lr, h->d_step ? 1 : h->step);
-    t.count = 0;
-    static const int kinds[3] = {FP_DTYPE_F32, FP_DTYPE_BF16, FP_DTYPE_F16};
-    cudaError_t e = cudaSuccess;
-    for (int pt : kinds)                                 // a launch has one type of each
-        for (int gt : kinds)
-            for (int bits = 8; bits <= 32; bits += 24) {
-                const Kernel k = kernel_of(pt, gt, bits);
-                const long long unit = bits == 32 ? kUnit32 : kUnit8;
-                long long units = 0;
-                for (int i = 0; i < count; ++i) {
-                    const fp_adamw_tensor& x = ts[i];
-                    if (x.n == 0 || x.p_dtype != pt || x.g_dtype != gt || x.state_bits != bits) continue;
-                    const long long mine = (x.n + unit - 1) / unit;
-                    if (t.count == kMaxTensors || units + mine > 0x7fffffffll) {
-                        if ((e = flush(t, (unsigned)units, k, (cudaStream_t)stream)) != cudaSuccess) goto done;
-                        units = 0;
-                    }
-                    Entry& r = t.e[t.count++];
-                    r.p = x.d_p; r.g = x.d_g; r.m = x.d_m; r.v = x.d_v; r.m_scale = x.d_m_scale; r.v_scale = x.d_v_scale;
-                    r.mask = x.d_mask; r.n = x.n; r.per_row = x.per_row; r.unit0 = (int)units;
-                    memset(&r.rows, 0, sizeof(r.rows));
-                    if (x.d_mask && x.n < (1ll << 31) && x.per_row < (1ll << 31)) r.rows = tc::make_fastdiv((uint32_t)x.per_row);
-                    const int vec = bits == 32 ? 4 : 16;
-                    r.aligned = multiple(x.d_p, std::min(16, vec * elem_bytes(pt))) && multiple(x.d_g, std::min(16, vec * elem_bytes(gt))) &&
-                                multiple(x.d_m, 16) && multiple(x.d_v, 16);
-                    units += mine;
-                }
-                if ((e = flush(t, (unsigned)units, k, (cudaStream_t)stream)) != cudaSuccess) goto done;
+    static const int dtypes[3] = {FP_DTYPE_F32, FP_DTYPE_BF16, FP_DTYPE_F16};
+    int left = 0;                                        // tensors that no launch has had yet
+    for (int i = 0; i < count; ++i) left += ts[i].n > 0;
+    for (int pt : dtypes)                                // a launch has one type of each
+        for (int gt : dtypes)
+            for (int bits = 8; bits <= 32 && left > 0; bits += 24) {
+                const Kind k = {pt, gt, bits};
+                int mine = 0;
+                for (int i = 0; i < count; ++i) mine += is_of(ts[i], k);
+                if (!mine) continue;
+                left -= mine;
+                const cudaError_t e = mine <= kFewTensors ? run_kind<kFewTensors>(s, ts, count, k, (cudaStream_t)stream)
+                                                          : run_kind<kMaxTensors>(s, ts, count, k, (cudaStream_t)stream);
+                if (e != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, cudaGetErrorString(e)); }
             }
-done:
-    if (e != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, cudaGetErrorString(e)); }
     return FP_OK;
 }
