@@ -84,18 +84,52 @@ __device__ __forceinline__ void store4(void* base, long long at, int dtype, cons
 
 // ---- activations ----------------------------------------------------------------------------------------------------
 // tanh(u) = 1 - 2 / (1 + e^2u), so z/2 (1 + tanh u) = z / (1 + e^-2u): one exponential, and no cancellation where the result is
-// small.  e^-2u = inf gives z / inf = 0, the limit.
+// small.  e^-2u = inf gives z * 0, the limit.  Exponentials and reciprocals are the approximate ones (2 ulp): results are rounded to
+// 16 bits, and the epilogue of a product has some 30 instructions an element before it, not the tensor cores, sets the pace.
 
 constexpr float kSqrt2OverPi2 = 1.5957691216057308f;       // 2 sqrt(2 / pi)
 constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 
+__device__ __forceinline__ float inverse(float x) {        // beyond 2^126: 0
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// Phi(z), with e = e^(-z^2 / 2) left for the density: Abramowitz and Stegun, formula 7.1.26, erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2)
+// with t = 1 / (1 + p x) for x >= 0, off by 1.5e-7 at most; below zero nothing cancels.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+    const float t = inverse(fmaf(0.3275911f * kInvSqrt2, fabsf(z), 1.0f));
+    e = __expf(-0.5f * z * z);
+    const float tail = 0.5f * e * t * fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
+    return z > 0.0f ? 1.0f - tail : tail;
+}
 __device__ __forceinline__ float act_of(float z, int act) {
     switch (act) {
         case FP_ACT_RELU: return z < 0.0f ? 0.0f : z;       // NaN stays
-        case FP_ACT_GELU: return 0.5f * z * (1.0f + erff(z * kInvSqrt2));
-        case FP_ACT_GELU_TANH: return z / (1.0f + __expf(-kSqrt2OverPi2 * (z + 0.044715f * z * z * z)));
-        case FP_ACT_SILU: return z / (1.0f + __expf(-z));
+        case FP_ACT_GELU: { float e; return z * normal_cdf(z, e); }
+        case FP_ACT_GELU_TANH: return z * inverse(1.0f + __expf(-kSqrt2OverPi2 * (z + 0.044715f * z * z * z)));
+        case FP_ACT_SILU: return z * inverse(1.0f + __expf(-z));
         default: return z;
+    }
+}
+__device__ __forceinline__ float act_grad(float z, int act) {
+    switch (act) {
+        case FP_ACT_RELU: return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
+        case FP_ACT_GELU: {
+            float e;
+            const float p = normal_cdf(z, e);
+            return fmaf(z * kInvSqrt2Pi, e, p);
+        }
+        case FP_ACT_GELU_TANH: {
+            // d/dz z s(2u) = s + z s (1 - s) 2u',  2u' = 2 sqrt(2/pi) (1 + 3 0.044715 z^2)
+            const float s = inverse(1.0f + __expf(-kSqrt2OverPi2 * (z + 0.044715f * z * z * z)));
+            return s + z * s * (1.0f - s) * kSqrt2OverPi2 * (1.0f + fminf(0.134145f * z * z, 1e30f));   // (0 times inf for a finite z)
+        }
+        case FP_ACT_SILU: {
+            const float s = inverse(1.0f + __expf(-z));
+            return s * (1.0f + z * (1.0f - s));
+        }
+        default: return 1.0f;
     }
 }
 // Rows of four values, the choice made once for all of them.
@@ -113,22 +147,5 @@ __device__ __forceinline__ void act_all(float (&v)[U][4], int act) {
     else if (act == FP_ACT_GELU_TANH) act_rows<FP_ACT_GELU_TANH>(v);
     else if (act == FP_ACT_SILU) act_rows<FP_ACT_SILU>(v);
 }
-__device__ __forceinline__ float act_grad(float z, int act) {
-    switch (act) {
-        case FP_ACT_RELU: return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
-        case FP_ACT_GELU: return 0.5f * (1.0f + erff(z * kInvSqrt2)) + z * kInvSqrt2Pi * __expf(-0.5f * z * z);
-        case FP_ACT_GELU_TANH: {
-            // d/dz z s(2u) = s + z s (1 - s) 2u',  2u' = 2 sqrt(2/pi) (1 + 3 0.044715 z^2)
-            const float s = 1.0f / (1.0f + __expf(-kSqrt2OverPi2 * (z + 0.044715f * z * z * z)));
-            return s + z * s * (1.0f - s) * kSqrt2OverPi2 * (1.0f + fminf(0.134145f * z * z, 1e30f));   // (0 times inf for a finite z)
-        }
-        case FP_ACT_SILU: {
-            const float s = 1.0f / (1.0f + __expf(-z));
-            return s * (1.0f + z * (1.0f - s));
-        }
-        default: return 1.0f;
-    }
-}
-
 }  // namespace train
 }  // namespace fp
