@@ -50,6 +50,7 @@ struct Problem {
 struct TileParams {
     Problem prob[2];
     int n_prob, stages, tiles;
+    int late;                                            // this launch's operands were there before the launch in front of it began: see after_the_last()
     uint32_t bf16;
     int* status;
 };
@@ -66,6 +67,17 @@ __device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity, volatil
         if (*abort_flag || clock64() - t0 > limit_cycles) return false;
     }
 }
+// Launches of these kernels overlap: each may begin while the one before it ends, prepares its barriers and tensor memory, and then
+// waits here for that one's results.  It lets the next one begin after that wait, so when the next one runs, all that was complete
+// before THIS launch is; a product that needs no more (the second of a call) is `late`: it waits only before it ends, so
+// that whatever follows it still follows both.
+__device__ __forceinline__ void after_the_last(int late) {
+    if (!late) asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+__device__ __forceinline__ void before_the_end(int late) {
+    if (late) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
 // Cycles after which a wait for a whole sum has run out: a block of 64 terms takes some hundred.
 __device__ __forceinline__ long long sum_limit(int kblocks) { return kWaitCycles + 4096ll * kblocks; }
 
@@ -81,11 +93,38 @@ __device__ __forceinline__ void bias4(const Epilogue& e, int n, int count, float
 #pragma unroll
     for (int i = 0; i < 4; ++i) b[i] = e.bias && i < count ? load1(e.bias, n + i, e.bias_type) : 0.0f;
 }
-// Outputs n .. n + count - 1 (up to four) of U rows `step` apart, those below `end`, from their sums and biases.  `e` is the caller's
-// own copy: its fields stay in registers.  Where four neighbours lie aligned everywhere, all that is read is asked for before anything is written.
+// Column n of U rows `step` apart, those below `end`, from their sums and its bias: what buffers take in which four neighbours do not lie
+// aligned, neighbouring lanes having neighbouring columns.  All that is read is asked for before anything is written.
+template <int U>
+__device__ __forceinline__ void finish_column(const Epilogue& e, long long row, int step, long long end, int n, float (&v)[U], float b) {
+    float r[U];
+    if (e.res)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (row + u * step < end) r[u] = load1(e.res, (row + u * step) * e.ld_res + n, e.res_type);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        v[u] += b;
+        if (e.res && e.res_first) v[u] += r[u];
+    }
+    if (e.pre)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (row + u * step < end) store1(e.pre, (row + u * step) * e.ld_pre + n, e.pre_type, v[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        v[u] = act_of(v[u], e.act);
+        if (e.res && !e.res_first) v[u] += r[u];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (row + u * step < end) store1(e.y, (row + u * step) * e.ld_y + n, e.y_type, v[u]);
+}
+// Outputs n .. n + count - 1 (up to four) of U rows `step` apart, those below `end`, from their sums and biases, where four neighbours lie
+// aligned in every buffer.
 template <int U>
 __device__ __forceinline__ void finish(const Epilogue& e, long long row, int step, long long end, int n, int count, float (&v)[U][4], const float (&b)[4]) {
-    if (e.vec && count == 4) {
+    if (count == 4) {
         float r[U][4];
         if (e.res)
 #pragma unroll
@@ -115,21 +154,12 @@ __device__ __forceinline__ void finish(const Epilogue& e, long long row, int ste
             if (row + u * step < end) store4(e.y, (row + u * step) * e.ld_y + n, e.y_type, v[u]);
         return;
     }
+#pragma unroll 1
+    for (int i = 0; i < count; ++i) {                    // the last columns of a matrix whose width is not a multiple of four
+        float one[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const long long at = row + u * step;
-        if (at >= end) break;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i >= count) break;
-            const float r = e.res ? load1(e.res, at * e.ld_res + n + i, e.res_type) : 0.0f;
-            float x = v[u][i] + b[i];
-            if (e.res && e.res_first) x += r;
-            if (e.pre) store1(e.pre, at * e.ld_pre + n + i, e.pre_type, x);
-            x = act_of(x, e.act);
-            if (e.res && !e.res_first) x += r;
-            store1(e.y, at * e.ld_y + n + i, e.y_type, x);
-        }
+        for (int u = 0; u < U; ++u) one[u] = i == 0 ? v[u][0] : i == 1 ? v[u][1] : v[u][2];
+        finish_column<U>(e, row, step, end, n + i, one, i == 0 ? b[0] : i == 1 ? b[1] : b[2]);
     }
 }
 __device__ __forceinline__ void lds16(uint32_t addr, float (&v)[4]) {
@@ -156,6 +186,71 @@ __device__ __forceinline__ void sums_of_parts(const uint32_t (&at)[U], uint32_t 
 #pragma unroll
             for (int s = 1; s < S; ++s) v[u][i] += part[u][s][i];
         }
+}
+
+template <int S, int U>
+__device__ __forceinline__ void sums_of_parts(const uint32_t (&at)[U], uint32_t first, uint32_t every, float (&v)[U]) {
+    float part[U][S];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int u = 0; u < U; ++u) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[u][s]) : "r"(cluster_addr(at[u], first + every * (uint32_t)s)));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        v[u] = part[u][0];
+#pragma unroll
+        for (int s = 1; s < S; ++s) v[u] += part[u][s];
+    }
+}
+// 128 columns of sums, finished by a warp: rows r0, r0 + step, ... below `rows` of those at `base` (pitch words apart), whose outputs
+// are rows row0 + r, columns n0 ..; the sum's S parts are in CTAs first, first + every, ...
+template <int S>
+__device__ __forceinline__ void finish_rows(const Epilogue& e, uint32_t base, int pitch, int r0, int step, int rows, long long row0, int n0, int N, uint32_t first,
+                                            uint32_t every) {
+    const int lane = threadIdx.x & 31;
+    if (e.vec) {
+        const int n = n0 + 4 * lane, count = min(4, N - n);
+        if (count <= 0) return;
+        float bias[4];
+        bias4(e, n, count, bias);
+        constexpr int U = S == 1 ? 4 : S >= 8 ? 1 : 8 / S;
+#pragma unroll 1
+        for (int r = r0; r < rows; r += U * step) {
+            float v[U][4];
+            uint32_t at[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) at[u] = base + (uint32_t)(min(r + u * step, rows - 1) * pitch + 4 * lane) * 4u;
+            if (S > 1) {
+                sums_of_parts<S, U>(at, first, every, v);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) lds16(at[u], v[u]);
+            }
+            finish<U>(e, row0 + r, step, row0 + rows, n, count, v, bias);
+        }
+        return;
+    }
+    constexpr int U = S >= 4 ? 4 : 8;
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+        const int n = n0 + 32 * c + lane;
+        if (n >= N) break;
+        const float bias = e.bias ? load1(e.bias, n, e.bias_type) : 0.0f;
+#pragma unroll 1
+        for (int r = r0; r < rows; r += U * step) {
+            float v[U];
+            uint32_t at[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) at[u] = base + (uint32_t)(min(r + u * step, rows - 1) * pitch + 32 * c + lane) * 4u;
+            if (S > 1) {
+                sums_of_parts<S, U>(at, first, every, v);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[u]) : "r"(at[u]));
+            }
+            finish_column<U>(e, row0 + r, step, row0 + rows, n, v, bias);
+        }
+    }
 }
 
 // ---- few rows: 128 outputs x BN rows a cluster ----------------------------------------------------------------------
@@ -203,6 +298,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctrl.tmem;
+    after_the_last(p.late);
     bool ok = true;
     if (warp == 0) {
         int stage = 0;
@@ -259,9 +355,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     // different banks.
     constexpr int kPitch = 132;
     const Epilogue e = held(q.e);
-    const int n = i0 + 4 * lane, count = min(4, q.I - n), rows = q.J;
-    float bias[4];
-    bias4(e, n, count, bias);
+    const int rows = q.J;
     {
         const int col = (warp & 3) * 32 + lane;
         const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
@@ -280,22 +374,15 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     tc_fence_before();
     if (S > 1) cluster_sync_all();
     else __syncthreads();
-    // warp w of CTA r finishes every (8 S)th row from 8 r + w on, four outputs a lane
-    if (count > 0)
-#pragma unroll 1
-        for (int r = (int)rank * 8 + warp; r < rows; r += 8 * S) {
-            const uint32_t at = base + (uint32_t)(r * kPitch + 4 * lane) * 4u;
-            float v[1][4];
-            if (S > 1) sums_of_parts<S, 1>({at}, 0u, 1u, v);
-            else lds16(at, v[0]);
-            finish<1>(e, r, 0, rows, n, count, v, bias);
-        }
+    finish_rows<S>(e, base, kPitch, (int)rank * 8 + warp, 8 * S, rows, 0, i0, q.I, 0u, 1u);      // (warp w of CTA r: every (8 S)th row from 8 r + w on)
+    __syncwarp();
     if (S > 1) cluster_sync_all();                        // no CTA leaves while another may still read its sums
     else __syncthreads();
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kCols) : "memory");
     }
+    before_the_end(p.late);
 }
 
 // ---- 256 x 256 tiles by CTA pairs -----------------------------------------------------------------------------------
@@ -363,6 +450,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = ctrl.tmem;
+    after_the_last(p.late);
     bool ok = true;
     if (warp == 0) {
         uint32_t stage = 0, phase = 0;
@@ -424,9 +512,9 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
             for (int c = 0; c < 4; ++c) {
                 uint32_t v[32];
                 tmem_ld32(tmem + ((uint32_t)(32 * quarter) << 16) + (n & 1) * 256u + (uint32_t)(half * 128 + 32 * c), v);
-                const int col = w.j0 + half * 128 + 32 * c + (lane & 7) * 4, count = min(4, w.q->J - col);
+                const int col0 = w.j0 + half * 128 + 32 * c, col = col0 + (e.vec ? (lane & 7) * 4 : lane), count = min(4, w.q->J - col);
                 float bias[4];
-                bias4(e, col, count, bias);
+                bias4(e, col, e.vec ? count : min(count, 1), bias);
                 tmem_ld_wait();
                 if (c == 3) {                            // the accumulator is free for the tile after the next
                     tc_fence_before();
@@ -436,7 +524,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
                 for (int i = 0; i < 8; ++i)
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(put + (uint32_t)i * 16u), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
                 __syncwarp();
-                if (count > 0)
+                if (count > 0 && e.vec) {
 #pragma unroll 1
                     for (int r = 0; r < 8; r += 4) {
                         float x[4][4];
@@ -444,6 +532,15 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
                         for (int u = 0; u < 4; ++u) lds16(get + (uint32_t)(4 * (r + u)) * (kEpiPitch * 4), x[u]);
                         finish<4>(e, row0 + 4 * r, 4, w.q->I, col, count, x, bias);
                     }
+                } else if (count > 0) {
+#pragma unroll 1
+                    for (int r = 0; r < 32; r += 8) {
+                        float x[8];
+#pragma unroll
+                        for (int u = 0; u < 8; ++u) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[u]) : "r"(buf + (uint32_t)((r + u) * kEpiPitch + lane) * 4u));
+                        finish_column<8>(e, row0 - (lane >> 3) + r, 1, w.q->I, col, x, bias[0]);
+                    }
+                }
                 __syncwarp();
             }
         }
@@ -457,6 +554,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
+    before_the_end(p.late);
 }
 
 // ---- 256 x 256 tiles with the sum split over pairs ----------------------------------------------------------------------
@@ -500,6 +598,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = ctrl.tmem;
+    after_the_last(p.late);
     bool ok = true;
     if (warp == 0) {
         uint32_t stage = 0, phase = 0;
@@ -560,40 +659,18 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
     tc_fence_before();
     if (S > 1) cluster_sync_all();
     else __syncthreads();
-    {
-        // Row r of this half of the tile is finished by warp r % 8 of pair (r / 8) % S, four outputs a lane and 128 further four more.
-        const Epilogue e = held(q.e);
-        const int rows = min(128, q.I - i0), step = 8 * S;
+    // Row r of this half of the tile is finished by warp r % 8 of pair (r / 8) % S.
+    const Epilogue e = held(q.e);
 #pragma unroll 1
-        for (int c = 0; c < 2; ++c) {
-            const int n = w.j0 + 128 * c + 4 * lane, count = min(4, q.J - n);
-            if (count <= 0) break;
-            float bias[4];
-            bias4(e, n, count, bias);
-            const uint32_t at0 = base + (uint32_t)(128 * c + 4 * lane) * 4u;
-            constexpr int U = S == 1 ? 4 : 8 / S;
-#pragma unroll 1
-            for (int r = split * 8 + warp; r < rows; r += U * step) {
-                float v[U][4];
-                uint32_t at[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) at[u] = at0 + (uint32_t)(min(r + u * step, rows - 1) * kSumPitch) * 4u;
-                if (S > 1) {
-                    sums_of_parts<S, U>(at, half, 2u, v);
-                } else {
-#pragma unroll
-                    for (int u = 0; u < U; ++u) lds16(at[u], v[u]);
-                }
-                finish<U>(e, (long long)i0 + r, step, (long long)i0 + rows, n, count, v, bias);
-            }
-        }
-    }
+    for (int c = 0; c < 2; ++c)
+        finish_rows<S>(e, base + 512u * (uint32_t)c, kSumPitch, split * 8 + warp, 8 * S, min(128, q.I - i0), i0, w.j0 + 128 * c, q.J, half, 2u);
     __syncwarp();
     cluster_sync_all();                                          // no CTA leaves while another may still read its sums or signal it
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
     }
+    before_the_end(p.late);
 }
 
 // ---- operands that tensor-map copies cannot read --------------------------------------------------------------------
@@ -610,6 +687,7 @@ struct CopyParams { CopyJob job[2]; long long warps; };
 // Rows of 16-bit elements of any alignment into rows that start at 16-byte boundaries.  A warp moves 512 elements, 64 bytes an
 // instruction: whatever the alignment the lines are used whole.
 __global__ void __launch_bounds__(256) copy_rows_kernel(const CopyParams p) {
+    after_the_last(0);
     const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (w >= p.warps) return;
     const CopyJob& j = p.job[w >= p.job[1].warp0 ? 1 : 0];
@@ -643,6 +721,7 @@ template <int DT, int ACT, bool VEC>
 __global__ void __launch_bounds__(256) linear_dz_kernel(const DzParams p) {
     __shared__ float part[16][128];
     __shared__ float sums[128];
+    after_the_last(0);
     const int lane = threadIdx.x & 15, half = threadIdx.x >> 4;
     const int split = (int)(blockIdx.x % (unsigned)p.splits);
     const int n0 = (int)(blockIdx.x / (unsigned)p.splits) * 128;
@@ -803,22 +882,29 @@ bool lay_out(const Product* prod, int n, int ti, int tj, int dtype, TileParams* 
     return true;
 }
 
-template <typename K>
-cudaError_t launch_clusters(K kernel, const TileParams& p, int blocks, int threads, int smem, int cluster, cudaStream_t st) {
+// A launch in clusters that may begin while the launch before it ends (see after_the_last).
+template <typename K, typename P>
+cudaError_t launch_clusters(K kernel, const P& p, long long blocks, int threads, int smem, int cluster, cudaStream_t st) {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)cluster;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
+
+// CTAs of linear_split_kernel that run at once in clusters of 2 S: a cluster lies within a group of SMs (B200: 148 in pairs, 132 in
+// fours, 120 in eights), and one cluster too many takes as long as all others (1024 x 1024 x 1024 in 16 clusters of eight 19.8 us, of four 11).
+int split_room(int S);
 
 template <int BN, int S>
 cudaError_t launch_tiles_of(const TileParams& p, int smem, cudaStream_t st) {
@@ -838,43 +924,93 @@ cudaError_t launch_split(const TileParams& p, cudaStream_t st) {
     return e != cudaSuccess ? e : launch_clusters(linear_split_kernel<S>, p, 2 * p.tiles * S, kSplitThreads, kSplitSmem, 2 * S, st);
 }
 
+constexpr int kMaxSplits = 4;
+int split_room(int S) {
+    static std::atomic<int> known[64][kMaxSplits + 1];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); dev = 0; }
+    int n = known[dev][S].load(std::memory_order_acquire);
+    if (n == 0) {
+        cudaLaunchConfig_t cfg;
+        memset(&cfg, 0, sizeof(cfg));
+        cfg.gridDim = dim3((unsigned)(2 * S * 512));
+        cfg.blockDim = dim3(kSplitThreads);
+        cfg.dynamicSmemBytes = kSplitSmem;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)(2 * S);
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        if (cudaFuncSetAttribute(linear_split_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, linear_split_kernel<2>, &cfg) != cudaSuccess || n <= 0) {
+            cudaGetLastError();
+            n = 1;
+        }
+        n = std::min(2 * S * n, sm_count());
+        known[dev][S].store(n, std::memory_order_release);
+    }
+    return n;
+}
+
 fp_status launched(cudaError_t e) {
     if (e == cudaSuccess) return FP_OK;
     cudaGetLastError();
     return err(FP_ERR_CUDA, cudaGetErrorString(e));
 }
 
-// Up to two products in one launch.
-fp_status run_products(const Product* prod, int n, int dtype, int* status, cudaStream_t st) {
+// The products of a call (two, or one); `late`: their operands were there before the launch in front of them began.
+fp_status run_products(const Product* prod, int n, int dtype, int late, int* status, cudaStream_t st) {
+    const char* refused = "fp_linear: an operand's tensor map was refused, or there are too many tiles";
+    const int sms = sm_count();
     TileParams p;
     memset(&p, 0, sizeof(p));
     p.status = status; p.bf16 = dtype == FP_DTYPE_BF16;
-    const char* refused = "fp_linear: an operand's tensor map was refused, or there are too many tiles";
-    const int sms = sm_count();
-    int splits = 1;
-    if (prod[0].swap) {
-        const int bn = prod[0].J <= 16 ? 16 : prod[0].J <= 32 ? 32 : prod[0].J <= 64 ? 64 : 128;
-        if (!lay_out(prod, n, 128, bn, dtype, &p)) return err(FP_ERR_CUDA, refused);
-        const int kblocks = p.prob[0].kblocks;
-        while (splits < 8 && p.tiles * splits * 2 <= sms && kblocks >= splits * 4) splits *= 2;
-        const int stage = 128 * 128 + bn * 128, room = p.tiles * splits > sms ? kMaxSmem / 2 - 3072 : kMaxSmem - 3072;
-        p.stages = std::min(std::min(room / stage, 16), (kblocks + splits - 1) / splits);
-        const int smem = std::max(p.stages * stage, bn * 132 * 4) + 1024;
-        return launched(bn == 16 ? launch_tiles<16>(p, splits, smem, st) : bn == 32 ? launch_tiles<32>(p, splits, smem, st)
-                        : bn == 64 ? launch_tiles<64>(p, splits, smem, st) : launch_tiles<128>(p, splits, smem, st));
+    bool few = prod[0].swap;
+    int64_t tiles[2] = {0, 0}, work = 0;
+    for (int i = 0; i < n; ++i) {
+        few = few || prod[i].swap;
+        tiles[i] = ((prod[i].I + 255) / 256) * ((prod[i].J + 255) / 256);
+        work += tiles[i] * ((prod[i].Kc + kBlockK - 1) / kBlockK);
     }
-    if (!lay_out(prod, n, 256, 256, dtype, &p)) return err(FP_ERR_CUDA, refused);
-    if (p.tiles > sms / 2) {
+    if (!few && tiles[0] + tiles[1] > sms / 2) {
         static std::atomic<unsigned long long> done;
+        if (!lay_out(prod, n, 256, 256, dtype, &p)) return err(FP_ERR_CUDA, refused);
+        p.late = late;
         const cudaError_t e = allow_smem(linear_pair_kernel, kPairSmem, &done);
         return launched(e != cudaSuccess ? e : launch_clusters(linear_pair_kernel, p, 2 * (sms / 2), kPairThreads, kPairSmem, 2, st));
     }
-    int kblocks = p.prob[0].kblocks;
-    if (n > 1) kblocks = std::min(kblocks, p.prob[1].kblocks);
-    // A cluster lies within a group of SMs: of 148, clusters of four CTAs reach 132, of eight 120 - and one cluster too many takes as
-    // long as all others (1024 x 1024 x 1024 in 16 clusters of eight 19.8 us).
-    while (splits < 4 && 2 * p.tiles * splits * 2 <= (splits == 1 ? sms * 132 / 148 : sms * 120 / 148) && kblocks >= splits * 4) splits *= 2;
-    return launched(splits == 1 ? launch_split<1>(p, st) : splits == 2 ? launch_split<2>(p, st) : launch_split<4>(p, st));
+    // one after the other, the second beside the first
+    for (int i = 0; i < n; ++i) {
+        fp_status s;
+        p.late = late || i > 0;
+        if (prod[i].swap) {
+            const int bn = prod[i].J <= 16 ? 16 : prod[i].J <= 32 ? 32 : prod[i].J <= 64 ? 64 : 128;
+            if (!lay_out(prod + i, 1, 128, bn, dtype, &p)) return err(FP_ERR_CUDA, refused);
+            const int kblocks = p.prob[0].kblocks;
+            int splits = 1;
+            while (splits < 8 && p.tiles * splits * 2 <= sms && kblocks >= splits * 4) splits *= 2;
+            const int stage = 128 * 128 + bn * 128, room = p.tiles * splits > sms ? kMaxSmem / 2 - 3072 : kMaxSmem - 3072;
+            p.stages = std::min(std::min(room / stage, 16), (kblocks + splits - 1) / splits);
+            const int smem = std::max(p.stages * stage, bn * 132 * 4) + 1024;
+            s = launched(bn == 16 ? launch_tiles<16>(p, splits, smem, st) : bn == 32 ? launch_tiles<32>(p, splits, smem, st)
+                         : bn == 64 ? launch_tiles<64>(p, splits, smem, st) : launch_tiles<128>(p, splits, smem, st));
+        } else if (tiles[i] > sms / 2) {
+            static std::atomic<unsigned long long> done;
+            if (!lay_out(prod + i, 1, 256, 256, dtype, &p)) return err(FP_ERR_CUDA, refused);
+            const cudaError_t e = allow_smem(linear_pair_kernel, kPairSmem, &done);
+            s = launched(e != cudaSuccess ? e : launch_clusters(linear_pair_kernel, p, 2 * (sms / 2), kPairThreads, kPairSmem, 2, st));
+        } else {
+            if (!lay_out(prod + i, 1, 256, 256, dtype, &p)) return err(FP_ERR_CUDA, refused);
+            // as many pairs a tile as its share of the SMs has room for, four K blocks a pair at least
+            const int kblocks = p.prob[0].kblocks, share = n > 1 && !few ? (int)(sms * tiles[i] * kblocks / work) : sms;
+            int S = kMaxSplits;
+            while (S > 1 && (2 * p.tiles * S > std::min(share, split_room(S)) || kblocks < 4 * S)) --S;
+            s = launched(S == 1 ? launch_split<1>(p, st) : S == 2 ? launch_split<2>(p, st) : S == 3 ? launch_split<3>(p, st) : launch_split<4>(p, st));
+        }
+        if (s != FP_OK) return s;
+    }
+    return FP_OK;
 }
 
 fp_status copy_rows(const CopyJob* jobs, int n, cudaStream_t st) {
@@ -888,9 +1024,7 @@ fp_status copy_rows(const CopyJob* jobs, int n, cudaStream_t st) {
         p.warps += p.job[i].rows * p.job[i].chunks;
     }
     if ((p.warps + 7) / 8 > 0x7fffffffll) return err(FP_ERR_BOUNDS, "fp_linear: operand too large");
-    copy_rows_kernel<<<(unsigned)((p.warps + 7) / 8), 256, 0, st>>>(p);
-    const cudaError_t e = cudaGetLastError();
-    return e == cudaSuccess ? FP_OK : err(FP_ERR_CUDA, cudaGetErrorString(e));
+    return launched(launch_clusters(copy_rows_kernel, p, (p.warps + 7) / 8, 256, 0, 1, st));
 }
 
 // Takes an operand into scratch where it cannot be read in place.
@@ -1030,7 +1164,7 @@ extern "C" fp_status fp_linear_forward(const fp_linear_args* a, void* work, size
     e.y_type = a->y_dtype; e.pre_type = e.res_type = a->dtype; e.bias_type = a->bias_dtype; e.act = a->act; e.res_first = a->res_first;
     e.vec = aligned4(a->d_y, a->ld_y, a->y_dtype, a->M) && (!a->d_pre || aligned4(a->d_pre, a->ld_pre, a->dtype, a->M)) &&
             (!a->d_res || aligned4(a->d_res, a->ld_res, a->dtype, a->M));
-    return run_products(&p, 1, a->dtype, status, st);
+    return run_products(&p, 1, a->dtype, 0, status, st);
 }
 
 extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work, size_t work_bytes, void* stream) {
@@ -1078,19 +1212,8 @@ extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work
         while (d.splits < 8 && a->M > 32 * d.splits && blocks * d.splits < 8 * sm_count()) d.splits *= 2;
         const bool vec = (a->N & 7) == 0 && readable(a->d_dy, a->M, a->ld_dy) && (a->act == FP_ACT_NONE || readable(a->d_pre, a->M, a->ld_pre)) &&
                          (!a->d_dz || readable(a->d_dz, a->M, a->ld_dz));
-        cudaLaunchConfig_t cfg;
-        memset(&cfg, 0, sizeof(cfg));
-        cfg.gridDim = dim3((unsigned)(blocks * d.splits));
-        cfg.blockDim = dim3(256);
-        cfg.stream = st;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)d.splits;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, a->dtype == FP_DTYPE_BF16 ? dz_kernel<FP_DTYPE_BF16>(a->act, vec) : dz_kernel<FP_DTYPE_F16>(a->act, vec), d);
-        if (e != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, cudaGetErrorString(e)); }
+        const DzKernel k = a->dtype == FP_DTYPE_BF16 ? dz_kernel<FP_DTYPE_BF16>(a->act, vec) : dz_kernel<FP_DTYPE_F16>(a->act, vec);
+        if ((s = launched(launch_clusters(k, d, blocks * d.splits, 256, 0, d.splits, st))) != FP_OK) return s;
     }
     if (!a->d_dx && !a->d_dw) return FP_OK;
     CopyJob jobs[2];
@@ -1109,10 +1232,6 @@ extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work
         r.I = r.swap ? a->K : a->M; r.J = r.swap ? a->M : a->K; r.Kc = a->N;
         r.e.y = a->d_dx; r.e.ld_y = a->ld_dx; r.e.y_type = a->dtype;
         r.e.vec = aligned4(a->d_dx, a->ld_dx, a->dtype, a->M);
-        if (r.swap) {
-            if ((s = run_products(p, 1, a->dtype, status, st)) != FP_OK) return s;
-            n = 0;
-        }
     }
     if (a->d_dw) {
         Product& r = p[n++];
@@ -1123,7 +1242,9 @@ extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work
         if (a->accumulate) { r.e.res = a->d_dw; r.e.ld_res = a->ld_dw; r.e.res_type = a->dw_dtype; }
         r.e.vec = aligned4(a->d_dw, a->ld_dw, a->dw_dtype, a->N);
     }
-    return n ? run_products(p, n, a->dtype, status, st) : FP_OK;
+    // Where a launch in front of the products only sums dz's columns, they need not wait for it.
+    const int late = a->d_db && !d.out[0] && !d.out[1] && !n_jobs;
+    return run_products(p, n, a->dtype, late, status, st);
 }
 
 extern "C" fp_status fp_linear_status(int32_t* out) {
