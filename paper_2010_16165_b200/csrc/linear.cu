@@ -89,167 +89,112 @@ __device__ __forceinline__ Epilogue held(const Epilogue& from) {
     asm volatile("" : "+r"(e.y_type), "+r"(e.pre_type), "+r"(e.res_type), "+r"(e.bias_type), "+r"(e.act), "+r"(e.res_first), "+r"(e.vec));
     return e;
 }
-__device__ __forceinline__ void bias4(const Epilogue& e, int n, int count, float (&b)[4]) {
+// A lane's four outputs of a row: neighbours n .. n + 3 where four neighbours lie aligned in every buffer (VEC), or else n, n + 32, n + 64 and
+// n + 96, so that neighbouring lanes have neighbouring columns.
+template <bool VEC> __device__ __forceinline__ int column(int n, int i) { return VEC ? n + i : n + 32 * i; }
+
+template <bool VEC>
+__device__ __forceinline__ void bias4(const Epilogue& e, int n, int N, float (&b)[4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = e.bias && i < count ? load1(e.bias, n + i, e.bias_type) : 0.0f;
+    for (int i = 0; i < 4; ++i) b[i] = e.bias && column<VEC>(n, i) < N ? load1(e.bias, column<VEC>(n, i), e.bias_type) : 0.0f;
 }
-// Column n of U rows `step` apart, those below `end`, from their sums and its bias: what buffers take in which four neighbours do not lie
-// aligned, neighbouring lanes having neighbouring columns.  All that is read is asked for before anything is written.
-template <int U>
-__device__ __forceinline__ void finish_column(const Epilogue& e, long long row, int step, long long end, int n, float (&v)[U], float b) {
-    float r[U];
-    if (e.res)
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (row + u * step < end) r[u] = load1(e.res, (row + u * step) * e.ld_res + n, e.res_type);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        v[u] += b;
-        if (e.res && e.res_first) v[u] += r[u];
-    }
-    if (e.pre)
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (row + u * step < end) store1(e.pre, (row + u * step) * e.ld_pre + n, e.pre_type, v[u]);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        v[u] = act_of(v[u], e.act);
-        if (e.res && !e.res_first) v[u] += r[u];
-    }
+// The residual of U rows `step` apart, those below `end`.
+template <int U, bool VEC>
+__device__ __forceinline__ void fetch(const Epilogue& e, long long row, int step, long long end, int n, int N, float (&r)[U][4]) {
+    if (!e.res) return;
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (row + u * step < end) store1(e.y, (row + u * step) * e.ld_y + n, e.y_type, v[u]);
+        if (row + u * step < end) {
+            const long long at = (row + u * step) * e.ld_res;
+            if (VEC && n + 4 <= N) load4(e.res, at + n, e.res_type, r[u]);
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i) if (column<VEC>(n, i) < N) r[u][i] = load1(e.res, at + column<VEC>(n, i), e.res_type);
+        }
 }
-// Outputs n .. n + count - 1 (up to four) of U rows `step` apart, those below `end`, from their sums and biases, where four neighbours lie
-// aligned in every buffer.
-template <int U>
-__device__ __forceinline__ void finish(const Epilogue& e, long long row, int step, long long end, int n, int count, float (&v)[U][4], const float (&b)[4]) {
-    if (count == 4) {
-        float r[U][4];
-        if (e.res)
+template <int U, bool VEC>
+__device__ __forceinline__ void put(void* to, long long ld, int type, long long row, int step, long long end, int n, int N, const float (&v)[U][4]) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (row + u * step < end) load4(e.res, (row + u * step) * e.ld_res + n, e.res_type, r[u]);
+    for (int u = 0; u < U; ++u)
+        if (row + u * step < end) {
+            const long long at = (row + u * step) * ld;
+            if (VEC && n + 4 <= N) store4(to, at + n, type, v[u]);
+            else
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[u][i] += b[i];
-        if (e.res && e.res_first)
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[u][i] += r[u][i];
-        if (e.pre)
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (row + u * step < end) store4(e.pre, (row + u * step) * e.ld_pre + n, e.pre_type, v[u]);
-        act_all(v, e.act);
-        if (e.res && !e.res_first)
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[u][i] += r[u][i];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (row + u * step < end) store4(e.y, (row + u * step) * e.ld_y + n, e.y_type, v[u]);
-        return;
-    }
-#pragma unroll 1
-    for (int i = 0; i < count; ++i) {                    // the last columns of a matrix whose width is not a multiple of four
-        float one[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) one[u] = i == 0 ? v[u][0] : i == 1 ? v[u][1] : v[u][2];
-        finish_column<U>(e, row, step, end, n + i, one, i == 0 ? b[0] : i == 1 ? b[1] : b[2]);
-    }
+                for (int i = 0; i < 4; ++i) if (column<VEC>(n, i) < N) store1(to, at + column<VEC>(n, i), type, v[u][i]);
+        }
 }
-__device__ __forceinline__ void lds16(uint32_t addr, float (&v)[4]) {
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr));
-}
-__device__ __forceinline__ void lds16_cluster(uint32_t addr, float (&v)[4]) {
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr));
-}
-
-// The parts of U sums that S CTAs of a cluster (first, first + every, ...) hold in their shared memory, added in that order.  All are
-// asked for at once: another CTA's memory answers after a thousand cycles.
-template <int S, int U>
-__device__ __forceinline__ void sums_of_parts(const uint32_t (&at)[U], uint32_t first, uint32_t every, float (&v)[U][4]) {
-    float part[U][S][4];
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-        for (int u = 0; u < U; ++u) lds16_cluster(cluster_addr(at[u], first + every * (uint32_t)s), part[u][s]);
+// The outputs from their sums v, biases b and residuals r.  `e` is the caller's own copy: its fields stay in registers.
+template <int U, bool VEC>
+__device__ __forceinline__ void finish(const Epilogue& e, long long row, int step, long long end, int n, int N, float (&v)[U][4], const float (&b)[4], const float (&r)[U][4]) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            v[u][i] = part[u][0][i];
-#pragma unroll
-            for (int s = 1; s < S; ++s) v[u][i] += part[u][s][i];
+            v[u][i] += b[i];
+            if (e.res && e.res_first) v[u][i] += r[u][i];
         }
+    if (e.pre) put<U, VEC>(e.pre, e.ld_pre, e.pre_type, row, step, end, n, N, v);
+    act_all(v, e.act);
+    if (e.res && !e.res_first)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[u][i] += r[u][i];
+    put<U, VEC>(e.y, e.ld_y, e.y_type, row, step, end, n, N, v);
+}
+// Four words of a row of sums: neighbours, or every 32nd.
+template <bool VEC>
+__device__ __forceinline__ void lds4(uint32_t addr, float (&v)[4]) {
+    if (VEC) asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr));
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[i]) : "r"(addr + 128u * (uint32_t)i));
+}
+template <bool VEC>
+__device__ __forceinline__ void lds4_cluster(uint32_t addr, float (&v)[4]) {
+    if (VEC) asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr));
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[i]) : "r"(addr + 128u * (uint32_t)i));
 }
 
-template <int S, int U>
-__device__ __forceinline__ void sums_of_parts(const uint32_t (&at)[U], uint32_t first, uint32_t every, float (&v)[U]) {
-    float part[U][S];
-#pragma unroll
-    for (int s = 0; s < S; ++s)
-#pragma unroll
-        for (int u = 0; u < U; ++u) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part[u][s]) : "r"(cluster_addr(at[u], first + every * (uint32_t)s)));
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        v[u] = part[u][0];
-#pragma unroll
-        for (int s = 1; s < S; ++s) v[u] += part[u][s];
-    }
-}
-// 128 columns of sums, finished by a warp: rows r0, r0 + step, ... below `rows` of those at `base` (pitch words apart), whose outputs
-// are rows row0 + r, columns n0 ..; the sum's S parts are in CTAs first, first + every, ...
-template <int S>
+// 128 columns of sums (n0 .. of the outputs), finished by a warp: rows r0, r0 + step, ... below `rows` of those at `base` (pitch words apart), which
+// are rows row0 + r of the outputs; the sum's S parts are in the shared memory of CTAs first, first + every, ... of the cluster and are added in that order.  U rows
+// at once: another CTA's memory answers after a thousand cycles, as the residual's does.
+template <int S, int U, bool VEC>
 __device__ __forceinline__ void finish_rows(const Epilogue& e, uint32_t base, int pitch, int r0, int step, int rows, long long row0, int n0, int N, uint32_t first,
                                             uint32_t every) {
-    const int lane = threadIdx.x & 31;
-    if (e.vec) {
-        const int n = n0 + 4 * lane, count = min(4, N - n);
-        if (count <= 0) return;
-        float bias[4];
-        bias4(e, n, count, bias);
-        constexpr int U = S == 1 ? 4 : S >= 8 ? 1 : 8 / S;
+    const int lane = threadIdx.x & 31, n = n0 + (VEC ? 4 * lane : lane);
+    if (n >= N) return;
+    float bias[4];
+    bias4<VEC>(e, n, N, bias);
 #pragma unroll 1
-        for (int r = r0; r < rows; r += U * step) {
-            float v[U][4];
-            uint32_t at[U];
+    for (int r = r0; r < rows; r += U * step) {
+        float v[U][4], res[U][4];
+        fetch<U, VEC>(e, row0 + r, step, row0 + rows, n, N, res);
+        uint32_t at[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) at[u] = base + (uint32_t)(min(r + u * step, rows - 1) * pitch + 4 * lane) * 4u;
-            if (S > 1) {
-                sums_of_parts<S, U>(at, first, every, v);
-            } else {
+        for (int u = 0; u < U; ++u) at[u] = base + (uint32_t)(min(r + u * step, rows - 1) * pitch + (VEC ? 4 : 1) * lane) * 4u;
+        if (S > 1) {
+            float part[U][S][4];
 #pragma unroll
-                for (int u = 0; u < U; ++u) lds16(at[u], v[u]);
-            }
-            finish<U>(e, row0 + r, step, row0 + rows, n, count, v, bias);
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int u = 0; u < U; ++u) lds4_cluster<VEC>(cluster_addr(at[u], first + every * (uint32_t)s), part[u][s]);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[u][i] = part[u][0][i];
+#pragma unroll
+                    for (int s = 1; s < S; ++s) v[u][i] += part[u][s][i];
+                }
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) lds4<VEC>(at[u], v[u]);
         }
-        return;
-    }
-    constexpr int U = S >= 4 ? 4 : 8;
-#pragma unroll 1
-    for (int c = 0; c < 4; ++c) {
-        const int n = n0 + 32 * c + lane;
-        if (n >= N) break;
-        const float bias = e.bias ? load1(e.bias, n, e.bias_type) : 0.0f;
-#pragma unroll 1
-        for (int r = r0; r < rows; r += U * step) {
-            float v[U];
-            uint32_t at[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) at[u] = base + (uint32_t)(min(r + u * step, rows - 1) * pitch + 32 * c + lane) * 4u;
-            if (S > 1) {
-                sums_of_parts<S, U>(at, first, every, v);
-            } else {
-#pragma unroll
-                for (int u = 0; u < U; ++u) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[u]) : "r"(at[u]));
-            }
-            finish_column<U>(e, row0 + r, step, row0 + rows, n, v, bias);
-        }
+        finish<U, VEC>(e, row0 + r, step, row0 + rows, n, N, v, bias, res);
     }
 }
 
@@ -374,7 +319,10 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     tc_fence_before();
     if (S > 1) cluster_sync_all();
     else __syncthreads();
-    finish_rows<S>(e, base, kPitch, (int)rank * 8 + warp, 8 * S, rows, 0, i0, q.I, 0u, 1u);      // (warp w of CTA r: every (8 S)th row from 8 r + w on)
+    // warp w of CTA r: every (8 S)th row from 8 r + w on
+    constexpr int U = S >= 8 || BN < 32 ? 1 : S == 4 ? 2 : 4;
+    if (e.vec) finish_rows<S, U, true>(e, base, kPitch, (int)rank * 8 + warp, 8 * S, rows, 0, i0, q.I, 0u, 1u);
+    else finish_rows<S, U, false>(e, base, kPitch, (int)rank * 8 + warp, 8 * S, rows, 0, i0, q.I, 0u, 1u);
     __syncwarp();
     if (S > 1) cluster_sync_all();                        // no CTA leaves while another may still read its sums
     else __syncthreads();
@@ -402,6 +350,33 @@ struct PairCtrl {
     uint32_t tmem;
     int abort_flag;
 };
+
+// Column n of the rows row .. row + 7 below `end`, from sums kEpiPitch words apart.
+__device__ __forceinline__ void finish_column(const Epilogue& e, long long row, long long end, int n, uint32_t from, float bias) {
+    float v[8], r[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        if (e.res && row + u < end) r[u] = load1(e.res, (row + u) * e.ld_res + n, e.res_type);
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[u]) : "r"(from + (uint32_t)(u * kEpiPitch) * 4u));
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        v[u] += bias;
+        if (e.res && e.res_first) v[u] += r[u];
+    }
+    if (e.pre)
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (row + u < end) store1(e.pre, (row + u) * e.ld_pre + n, e.pre_type, v[u]);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        v[u] = act_of(v[u], e.act);
+        if (e.res && !e.res_first) v[u] += r[u];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+        if (row + u < end) store1(e.y, (row + u) * e.ld_y + n, e.y_type, v[u]);
+}
 
 struct Place { const Problem* q; int i0, j0; };
 __device__ __forceinline__ Place pair_place(const TileParams& p, int tile_all) {
@@ -507,14 +482,12 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
             ok = __all_sync(0xffffffffu, mbar_poll(sums_full + 8 * (n & 1), (n >> 1) & 1u, abort_flag, sum_limit(w.q->kblocks)));
             if (!ok) break;
             tc_fence_after();
-            const int row0 = w.i0 + 128 * (int)rank + 32 * quarter + (lane >> 3);
+            const int row0 = w.i0 + 128 * (int)rank + 32 * quarter;
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
                 uint32_t v[32];
                 tmem_ld32(tmem + ((uint32_t)(32 * quarter) << 16) + (n & 1) * 256u + (uint32_t)(half * 128 + 32 * c), v);
-                const int col0 = w.j0 + half * 128 + 32 * c, col = col0 + (e.vec ? (lane & 7) * 4 : lane), count = min(4, w.q->J - col);
-                float bias[4];
-                bias4(e, col, e.vec ? count : min(count, 1), bias);
+                const int col0 = w.j0 + half * 128 + 32 * c;
                 tmem_ld_wait();
                 if (c == 3) {                            // the accumulator is free for the tile after the next
                     tc_fence_before();
@@ -524,22 +497,25 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
                 for (int i = 0; i < 8; ++i)
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(put + (uint32_t)i * 16u), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
                 __syncwarp();
-                if (count > 0 && e.vec) {
+                if (e.vec) {                             // four rows at a time, eight lanes a row
+                    const int n = col0 + (lane & 7) * 4;
+                    if (n < w.q->J) {
+                        float bias[4];
+                        bias4<true>(e, n, w.q->J, bias);
 #pragma unroll 1
-                    for (int r = 0; r < 8; r += 4) {
-                        float x[4][4];
+                        for (int r = 0; r < 8; r += 4) {
+                            float x[4][4], res[4][4];
+                            fetch<4, true>(e, row0 + (lane >> 3) + 4 * r, 4, w.q->I, n, w.q->J, res);
 #pragma unroll
-                        for (int u = 0; u < 4; ++u) lds16(get + (uint32_t)(4 * (r + u)) * (kEpiPitch * 4), x[u]);
-                        finish<4>(e, row0 + 4 * r, 4, w.q->I, col, count, x, bias);
+                            for (int u = 0; u < 4; ++u) lds4<true>(get + (uint32_t)(4 * (r + u)) * (kEpiPitch * 4), x[u]);
+                            finish<4, true>(e, row0 + (lane >> 3) + 4 * r, 4, w.q->I, n, w.q->J, x, bias, res);
+                        }
                     }
-                } else if (count > 0) {
+                } else if (col0 + lane < w.q->J) {       // a lane a column, four rows in the places of four columns
+                    const int n = col0 + lane;
+                    const float bias = e.bias ? load1(e.bias, n, e.bias_type) : 0.0f;
 #pragma unroll 1
-                    for (int r = 0; r < 32; r += 8) {
-                        float x[8];
-#pragma unroll
-                        for (int u = 0; u < 8; ++u) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[u]) : "r"(buf + (uint32_t)((r + u) * kEpiPitch + lane) * 4u));
-                        finish_column<8>(e, row0 - (lane >> 3) + r, 1, w.q->I, col, x, bias[0]);
-                    }
+                    for (int r = 0; r < 32; r += 8) finish_column(e, row0 + r, w.q->I, n, buf + (uint32_t)(r * kEpiPitch + lane) * 4u, bias);
                 }
                 __syncwarp();
             }
@@ -562,7 +538,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
 // An SM takes 64 bytes a cycle from L2, so tiles are what counts: 32 KB a K block for 512 cycles of the tensor cores here; 128 x 128
 // tiles of single CTAs need the same 32 KB for 256 cycles' work and ran at half the rate however they were spread.
 
-constexpr int kSplitThreads = 256, kSumPitch = 260;      // words of a row of sums: 16-byte accesses of neighbouring lanes in different banks
+constexpr int kSplitThreads = 512, kSumPitch = 260;      // words of a row of sums: 16-byte accesses of neighbouring lanes in different banks
 constexpr int kSplitSmem = kPairStages * (int)kPairStage + 1024;
 static_assert(128 * kSumPitch * 4 <= kPairStages * (int)kPairStage, "the sums take the stages' memory");
 
@@ -644,10 +620,10 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
         for (int i = 0; i < 200; ++i) __nanosleep(1000);         // copies in flight land before the memory is used again
     __syncthreads();                                             // every stage has been read: its memory takes the sums now
     {
-        const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * 128);
-        const uint32_t to = base + (uint32_t)(((warp & 3) * 32 + lane) * kSumPitch + (warp >> 2) * 128) * 4u;
-#pragma unroll 2
-        for (int c = 0; c < 4; ++c) {
+        const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * 64);
+        const uint32_t to = base + (uint32_t)(((warp & 3) * 32 + lane) * kSumPitch + (warp >> 2) * 64) * 4u;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
             uint32_t v[32];
             tmem_ld32(taddr + (uint32_t)(32 * c), v);
             tmem_ld_wait();
@@ -659,11 +635,16 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
     tc_fence_before();
     if (S > 1) cluster_sync_all();
     else __syncthreads();
-    // Row r of this half of the tile is finished by warp r % 8 of pair (r / 8) % S.
+    // Row r of this half of the tile is finished by warp r % 16 of pair (r / 16) % S.
     const Epilogue e = held(q.e);
+    constexpr int U = S == 3 ? 3 : 8 / S < 4 ? 8 / S : 4;
 #pragma unroll 1
-    for (int c = 0; c < 2; ++c)
-        finish_rows<S>(e, base + 512u * (uint32_t)c, kSumPitch, split * 8 + warp, 8 * S, min(128, q.I - i0), i0, w.j0 + 128 * c, q.J, half, 2u);
+    for (int c = 0; c < 2; ++c) {
+        const uint32_t from = base + 512u * (uint32_t)c;
+        const int rows = min(128, q.I - i0), n0 = w.j0 + 128 * c;
+        if (e.vec) finish_rows<S, U, true>(e, from, kSumPitch, split * 16 + warp, 16 * S, rows, i0, n0, q.J, half, 2u);
+        else finish_rows<S, U, false>(e, from, kSumPitch, split * 16 + warp, 16 * S, rows, i0, n0, q.J, half, 2u);
+    }
     __syncwarp();
     cluster_sync_all();                                          // no CTA leaves while another may still read its sums or signal it
     if (warp == 1) {
@@ -686,7 +667,7 @@ struct CopyParams { CopyJob job[2]; long long warps; };
 
 // Rows of 16-bit elements of any alignment into rows that start at 16-byte boundaries.  A warp moves 512 elements, 64 bytes an
 // instruction: whatever the alignment the lines are used whole.
-__global__ void __launch_bounds__(256) copy_rows_kernel(const CopyParams p) {
+__global__ void __launch_bounds__(256) copy_rows_kernel(const __grid_constant__ CopyParams p) {
     after_the_last(0);
     const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (w >= p.warps) return;
