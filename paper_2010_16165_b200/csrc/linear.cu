@@ -169,10 +169,7 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, uint32_t base, in
     if (n >= N) return;
     float bias[4];
     bias4<VEC>(e, n, N, bias);
-#pragma unroll 1
-    for (int r = r0; r < rows; r += U * step) {
-        float v[U][4], res[U][4];
-        fetch<U, VEC>(e, row0 + r, step, row0 + rows, n, N, res);
+    auto sums = [&](int r, float (&v)[U][4]) {
         uint32_t at[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) at[u] = base + (uint32_t)(min(r + u * step, rows - 1) * pitch + (VEC ? 4 : 1) * lane) * 4u;
@@ -194,6 +191,30 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, uint32_t base, in
 #pragma unroll
             for (int u = 0; u < U; ++u) lds4<VEC>(at[u], v[u]);
         }
+    };
+    if (VEC && n + 4 <= N && !e.res && !e.pre && e.act == FP_ACT_NONE) {       // nothing but a bias: a gradient, or logits
+        const int bytes = e.y_type == FP_DTYPE_F32 ? 4 : 2;
+        char* to = static_cast<char*>(e.y) + ((row0 + r0) * e.ld_y + n) * bytes;
+        const long long hop = step * e.ld_y * bytes;
+#pragma unroll 1
+        for (int r = r0; r < rows; r += U * step) {
+            float v[U][4];
+            sums(r, v);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[u][i] += bias[i];
+                if (r + u * step < rows) store4(to, 0, e.y_type, v[u]);
+                to += hop;
+            }
+        }
+        return;
+    }
+#pragma unroll 1
+    for (int r = r0; r < rows; r += U * step) {
+        float v[U][4], res[U][4];
+        fetch<U, VEC>(e, row0 + r, step, row0 + rows, n, N, res);
+        sums(r, v);
         finish<U, VEC>(e, row0 + r, step, row0 + rows, n, N, v, bias, res);
     }
 }
@@ -379,21 +400,23 @@ __device__ __forceinline__ void finish_column(const Epilogue& e, long long row, 
 }
 
 struct Place { const Problem* q; int i0, j0; };
+template <int BN>
 __device__ __forceinline__ Place pair_place(const TileParams& p, int tile_all) {
     Place r;
     r.q = &p.prob[p.n_prob > 1 && tile_all >= p.prob[1].tile0 ? 1 : 0];
     const int tile = tile_all - r.q->tile0;
     const int group = tile / (8 * r.q->tiles_j), in_group = tile - group * 8 * r.q->tiles_j, rows_here = min(8, r.q->tiles_i - group * 8);
     r.i0 = (group * 8 + in_group % rows_here) * 256;
-    r.j0 = (in_group / rows_here) * 256;
+    r.j0 = (in_group / rows_here) * BN;
     return r;
 }
 
-// 128 rows of an operand (from row0 on, 64 terms of the sum from k on) into this CTA's stage.
+// ROWS rows of an operand (from row0 on, 64 terms of the sum from k on) into this CTA's stage.
+template <int ROWS>
 __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap& map, int mn, int row0, int k, uint32_t bar) {
     if (mn) {
         tma_load_2d_pair(dst, &map, row0, k, bar);
-        tma_load_2d_pair(dst + 8192, &map, row0 + 64, k, bar);
+        if (ROWS > 64) tma_load_2d_pair(dst + 8192, &map, row0 + 64, k, bar);
     } else {
         tma_load_2d_pair(dst, &map, k, row0, bar);
     }
@@ -431,7 +454,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
         uint32_t stage = 0, phase = 0;
         bool again = false;                              // whether the ring has come round
         for (int t = pair; t < p.tiles && ok; t += pairs) {
-            const Place w = pair_place(p, t);
+            const Place w = pair_place<256>(p, t);
             const int i0 = w.i0 + 128 * (int)rank, j0 = w.j0 + 128 * (int)rank;
             for (int kb = 0; kb < w.q->kblocks; ++kb) {
                 if (again) ok = __all_sync(0xffffffffu, mbar_poll(empty0 + 8 * stage, phase ^ 1u, abort_flag));
@@ -439,8 +462,8 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
                 if (elect_one()) {
                     const uint32_t own = full0 + 8 * stage, bar = cluster_addr(own, 0), a = base + stage * kPairStage;
                     if (rank == 0) mbar_expect_tx(own, 2 * kPairStage);
-                    load_rows(a, w.q->a, w.q->a_mn, i0, kb * kBlockK, bar);
-                    load_rows(a + 128 * 128, w.q->b, w.q->b_mn, j0, kb * kBlockK, bar);
+                    load_rows<128>(a, w.q->a, w.q->a_mn, i0, kb * kBlockK, bar);
+                    load_rows<128>(a + 128 * 128, w.q->b, w.q->b_mn, j0, kb * kBlockK, bar);
                 }
                 __syncwarp();
                 if (++stage == kPairStages) { stage = 0; phase ^= 1u; again = true; }
@@ -449,7 +472,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
     } else if (warp == 1 && rank == 0) {
         uint32_t stage = 0, phase = 0, n = 0;
         for (int t = pair; t < p.tiles && ok; t += pairs, ++n) {
-            const Place w = pair_place(p, t);
+            const Place w = pair_place<256>(p, t);
             const uint32_t idesc = f16_idesc((int)p.bf16, w.q->a_mn, w.q->b_mn, 256, 256);
             const uint32_t a_step = w.q->a_mn ? 128u : 2u, b_step = w.q->b_mn ? 128u : 2u, d = tmem + (n & 1) * 256u;
             if (n >= 2) ok = __all_sync(0xffffffffu, mbar_poll(sums_empty + 8 * (n & 1), ((n >> 1) & 1u) ^ 1u, abort_flag));
@@ -477,7 +500,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
         const uint32_t put = buf + (uint32_t)lane * (kEpiPitch * 4), get = buf + (uint32_t)(lane >> 3) * (kEpiPitch * 4) + (uint32_t)(lane & 7) * 16u;
         uint32_t n = 0;
         for (int t = pair; t < p.tiles; t += pairs, ++n) {
-            const Place w = pair_place(p, t);
+            const Place w = pair_place<256>(p, t);
             const Epilogue e = held(w.q->e);
             ok = __all_sync(0xffffffffu, mbar_poll(sums_full + 8 * (n & 1), (n >> 1) & 1u, abort_flag, sum_limit(w.q->kblocks)));
             if (!ok) break;
@@ -533,41 +556,54 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
     before_the_end(p.late);
 }
 
-// ---- 256 x 256 tiles with the sum split over pairs ----------------------------------------------------------------------
+// ---- 256 x BN tiles with the sum split over pairs -----------------------------------------------------------------------
 // Products of fewer tiles than there are pairs: S pairs (a cluster of 2 S CTAs) share a tile's sum, as with few rows.
-// An SM takes 64 bytes a cycle from L2, so tiles are what counts: 32 KB a K block for 512 cycles of the tensor cores here; 128 x 128
-// tiles of single CTAs need the same 32 KB for 256 cycles' work and ran at half the rate however they were spread.
+// An SM takes 64 bytes a cycle from L2, so tiles are what counts: 32 KB a K block for 512 cycles of the tensor cores at BN = 256, 24 KB (392
+// cycles measured) for 256 cycles' work at BN = 128; 128 x 128 tiles of single CTAs need 32 KB for 256 cycles' work and ran at half the
+// rate however they were spread.  Another CTA's sums come at 16 bytes a cycle, 4096 cycles for half a tile of 256 columns.
 
-constexpr int kSplitThreads = 512, kSumPitch = 260;      // words of a row of sums: 16-byte accesses of neighbouring lanes in different banks
-constexpr int kSplitSmem = kPairStages * (int)kPairStage + 1024;
-static_assert(128 * kSumPitch * 4 <= kPairStages * (int)kPairStage, "the sums take the stages' memory");
+constexpr int kSplitThreads = 512;
+template <int BN> struct SplitShape {
+    static constexpr int kStages = BN == 256 ? 5 : 7, kPitch = BN + 4;     // words of a row of sums: 16-byte accesses of neighbouring lanes in different banks
+    static constexpr uint32_t kStage = 128 * 128 + BN / 2 * 128;
+    static constexpr int kSmem = kStages * (int)kStage + 1024;
+    static_assert(128 * kPitch * 4 <= kStages * (int)kStage, "the sums take the stages' memory");
+};
+struct SplitCtrl {
+    uint64_t full[8], empty[8], done;
+    uint32_t tmem;
+    int abort_flag;
+};
 
-template <int S>
+template <int BN, int S>
 __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __grid_constant__ TileParams p) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ PairCtrl ctrl;
+    __shared__ SplitCtrl ctrl;
+    typedef SplitShape<BN> Shape;
+    constexpr int kStages = Shape::kStages;
+    constexpr uint32_t kStage = Shape::kStage;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), half = rank & 1u, first = rank & ~1u;      // this CTA's place in its pair, and the pair's first CTA
     const int split = (int)(rank >> 1);
-    const Place w = pair_place(p, (int)(blockIdx.x / (unsigned)(2 * S)));
+    const Place w = pair_place<BN>(p, (int)(blockIdx.x / (unsigned)(2 * S)));
     const Problem& q = *w.q;
     const int i0 = w.i0 + 128 * (int)half;
     const int kb0 = (int)((long long)q.kblocks * split / S), kb1 = (int)((long long)q.kblocks * (split + 1) / S);
     volatile int* abort_flag = &ctrl.abort_flag;
-    const uint32_t full0 = smem_u32(ctrl.full), empty0 = smem_u32(ctrl.empty), done = smem_u32(ctrl.sums_full);
+    const uint32_t full0 = smem_u32(ctrl.full), empty0 = smem_u32(ctrl.empty), done = smem_u32(&ctrl.done);
 
     if (warp == 0) {
         if (lane == 0) {
             prefetch_map(&q.a);
             prefetch_map(&q.b);
-            for (int s = 0; s < kPairStages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+            for (int s = 0; s < kStages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
             mbar_init(done, 1);
             ctrl.abort_flag = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
     } else if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl.tmem)), "r"(256u) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl.tmem)), "r"((uint32_t)BN) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
     tc_fence_before();
@@ -578,27 +614,27 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
     bool ok = true;
     if (warp == 0) {
         uint32_t stage = 0, phase = 0;
-        const int j0 = w.j0 + 128 * (int)half;
+        const int j0 = w.j0 + BN / 2 * (int)half;
         for (int kb = kb0; kb < kb1; ++kb) {
-            if (kb - kb0 >= kPairStages) ok = __all_sync(0xffffffffu, mbar_poll(empty0 + 8 * stage, phase ^ 1u, abort_flag));
+            if (kb - kb0 >= kStages) ok = __all_sync(0xffffffffu, mbar_poll(empty0 + 8 * stage, phase ^ 1u, abort_flag));
             if (!ok) break;
             if (elect_one()) {
-                const uint32_t own = full0 + 8 * stage, bar = cluster_addr(own, first), a = base + stage * kPairStage;
-                if (half == 0) mbar_expect_tx(own, 2 * kPairStage);
-                load_rows(a, q.a, q.a_mn, i0, kb * kBlockK, bar);
-                load_rows(a + 128 * 128, q.b, q.b_mn, j0, kb * kBlockK, bar);
+                const uint32_t own = full0 + 8 * stage, bar = cluster_addr(own, first), a = base + stage * kStage;
+                if (half == 0) mbar_expect_tx(own, 2 * kStage);
+                load_rows<128>(a, q.a, q.a_mn, i0, kb * kBlockK, bar);
+                load_rows<BN / 2>(a + 128 * 128, q.b, q.b_mn, j0, kb * kBlockK, bar);
             }
             __syncwarp();
-            if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
     } else if (warp == 1 && half == 0) {
         uint32_t stage = 0, phase = 0;
-        const uint32_t idesc = f16_idesc((int)p.bf16, q.a_mn, q.b_mn, 256, 256), a_step = q.a_mn ? 128u : 2u, b_step = q.b_mn ? 128u : 2u;
+        const uint32_t idesc = f16_idesc((int)p.bf16, q.a_mn, q.b_mn, 256, BN), a_step = q.a_mn ? 128u : 2u, b_step = q.b_mn ? 128u : 2u;
         for (int kb = kb0; kb < kb1; ++kb) {
             ok = __all_sync(0xffffffffu, mbar_poll(full0 + 8 * stage, phase, abort_flag));
             if (!ok) break;
             tc_fence_after();
-            const uint32_t a = base + stage * kPairStage, al = sw128_lo(a, 8192), bl = sw128_lo(a + 128 * 128, 8192), leader = elect_one();
+            const uint32_t a = base + stage * kStage, al = sw128_lo(a, 8192), bl = sw128_lo(a + 128 * 128, 8192), leader = elect_one();
 #pragma unroll
             for (int s = 0; s < 4; ++s)
                 umma_sw128_pair_if(leader, tmem, al + (uint32_t)s * a_step, bl + (uint32_t)s * b_step, idesc, kb > kb0 || s ? 1u : 0u);
@@ -607,7 +643,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
                 if (kb == kb1 - 1) umma_commit_pair(done, first);
             }
             __syncwarp();
-            if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+            if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
     }
     if (!ok && lane == 0) { atomicExch(&ctrl.abort_flag, 1); atomicExch(p.status, 1); }
@@ -620,10 +656,11 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
         for (int i = 0; i < 200; ++i) __nanosleep(1000);         // copies in flight land before the memory is used again
     __syncthreads();                                             // every stage has been read: its memory takes the sums now
     {
-        const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * 64);
-        const uint32_t to = base + (uint32_t)(((warp & 3) * 32 + lane) * kSumPitch + (warp >> 2) * 64) * 4u;
+        constexpr int kCols = BN / 4;                    // a warp's columns
+        const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * kCols);
+        const uint32_t to = base + (uint32_t)(((warp & 3) * 32 + lane) * Shape::kPitch + (warp >> 2) * kCols) * 4u;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < kCols / 32; ++c) {
             uint32_t v[32];
             tmem_ld32(taddr + (uint32_t)(32 * c), v);
             tmem_ld_wait();
@@ -639,17 +676,17 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
     const Epilogue e = held(q.e);
     constexpr int U = S == 3 ? 3 : 8 / S < 4 ? 8 / S : 4;
 #pragma unroll 1
-    for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < BN / 128; ++c) {
         const uint32_t from = base + 512u * (uint32_t)c;
         const int rows = min(128, q.I - i0), n0 = w.j0 + 128 * c;
-        if (e.vec) finish_rows<S, U, true>(e, from, kSumPitch, split * 16 + warp, 16 * S, rows, i0, n0, q.J, half, 2u);
-        else finish_rows<S, U, false>(e, from, kSumPitch, split * 16 + warp, 16 * S, rows, i0, n0, q.J, half, 2u);
+        if (e.vec) finish_rows<S, U, true>(e, from, Shape::kPitch, split * 16 + warp, 16 * S, rows, i0, n0, q.J, half, 2u);
+        else finish_rows<S, U, false>(e, from, Shape::kPitch, split * 16 + warp, 16 * S, rows, i0, n0, q.J, half, 2u);
     }
     __syncwarp();
     cluster_sync_all();                                          // no CTA leaves while another may still read its sums or signal it
     if (warp == 1) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)BN) : "memory");
     }
     before_the_end(p.late);
 }
@@ -843,8 +880,8 @@ cudaError_t allow_smem(K kernel, int bytes, std::atomic<unsigned long long>* don
 struct Operand { const void* p; int64_t rows, cols, ld; int mn; };   // mn: rows are the sum's index
 struct Product { Operand a, b; int64_t I, J, Kc; int swap; Epilogue e; };
 
-// Fills in a launch's problems for tiles of ti x tj; false where a tensor map is refused, or there are more tiles than an index holds.
-bool lay_out(const Product* prod, int n, int ti, int tj, int dtype, TileParams* p) {
+// Fills in a launch's problems for tiles of ti x tj, B in boxes of box_b rows; false where a tensor map is refused, or there are more tiles than an index holds.
+bool lay_out(const Product* prod, int n, int ti, int tj, int box_b, int dtype, TileParams* p) {
     int64_t tiles = 0;
     for (int i = 0; i < n; ++i) {
         const Product& r = prod[i];
@@ -856,7 +893,7 @@ bool lay_out(const Product* prod, int n, int ti, int tj, int dtype, TileParams* 
         if (tiles > (1 << 27)) return false;
         q.a_mn = r.a.mn; q.b_mn = r.b.mn; q.e = r.e;
         if (!make_map(&q.a, r.a.p, r.a.rows, r.a.cols, r.a.ld, r.a.mn ? 64 : 128, dtype) ||
-            !make_map(&q.b, r.b.p, r.b.rows, r.b.cols, r.b.ld, r.b.mn ? 64 : std::min(tj, 128), dtype))
+            !make_map(&q.b, r.b.p, r.b.rows, r.b.cols, r.b.ld, r.b.mn ? 64 : box_b, dtype))
             return false;
     }
     p->n_prob = n; p->tiles = (int)tiles;
@@ -898,11 +935,15 @@ cudaError_t launch_tiles(const TileParams& p, int splits, int smem, cudaStream_t
     return splits == 1 ? launch_tiles_of<BN, 1>(p, smem, st) : splits == 2 ? launch_tiles_of<BN, 2>(p, smem, st)
          : splits == 4 ? launch_tiles_of<BN, 4>(p, smem, st) : launch_tiles_of<BN, 8>(p, smem, st);
 }
-template <int S>
-cudaError_t launch_split(const TileParams& p, cudaStream_t st) {
+template <int BN, int S>
+cudaError_t launch_split_of(const TileParams& p, cudaStream_t st) {
     static std::atomic<unsigned long long> done;
-    const cudaError_t e = allow_smem(linear_split_kernel<S>, kSplitSmem, &done);
-    return e != cudaSuccess ? e : launch_clusters(linear_split_kernel<S>, p, 2 * p.tiles * S, kSplitThreads, kSplitSmem, 2 * S, st);
+    const cudaError_t e = allow_smem(linear_split_kernel<BN, S>, SplitShape<BN>::kSmem, &done);
+    return e != cudaSuccess ? e : launch_clusters(linear_split_kernel<BN, S>, p, 2 * p.tiles * S, kSplitThreads, SplitShape<BN>::kSmem, 2 * S, st);
+}
+template <int BN>
+cudaError_t launch_split(const TileParams& p, int S, cudaStream_t st) {
+    return S == 1 ? launch_split_of<BN, 1>(p, st) : S == 2 ? launch_split_of<BN, 2>(p, st) : S == 3 ? launch_split_of<BN, 3>(p, st) : launch_split_of<BN, 4>(p, st);
 }
 
 constexpr int kMaxSplits = 4;
@@ -916,15 +957,15 @@ int split_room(int S) {
         memset(&cfg, 0, sizeof(cfg));
         cfg.gridDim = dim3((unsigned)(2 * S * 512));
         cfg.blockDim = dim3(kSplitThreads);
-        cfg.dynamicSmemBytes = kSplitSmem;
+        cfg.dynamicSmemBytes = SplitShape<256>::kSmem;
         cudaLaunchAttribute attr;
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = (unsigned)(2 * S);
         attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        if (cudaFuncSetAttribute(linear_split_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(&n, linear_split_kernel<2>, &cfg) != cudaSuccess || n <= 0) {
+        if (cudaFuncSetAttribute(linear_split_kernel<256, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, SplitShape<256>::kSmem) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&n, linear_split_kernel<256, 2>, &cfg) != cudaSuccess || n <= 0) {
             cudaGetLastError();
             n = 1;
         }
@@ -956,7 +997,7 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, int* sta
     }
     if (!few && tiles[0] + tiles[1] > sms / 2) {
         static std::atomic<unsigned long long> done;
-        if (!lay_out(prod, n, 256, 256, dtype, &p)) return err(FP_ERR_CUDA, refused);
+        if (!lay_out(prod, n, 256, 256, 128, dtype, &p)) return err(FP_ERR_CUDA, refused);
         p.late = late;
         const cudaError_t e = allow_smem(linear_pair_kernel, kPairSmem, &done);
         return launched(e != cudaSuccess ? e : launch_clusters(linear_pair_kernel, p, 2 * (sms / 2), kPairThreads, kPairSmem, 2, st));
@@ -967,7 +1008,7 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, int* sta
         p.late = late || i > 0;
         if (prod[i].swap) {
             const int bn = prod[i].J <= 16 ? 16 : prod[i].J <= 32 ? 32 : prod[i].J <= 64 ? 64 : 128;
-            if (!lay_out(prod + i, 1, 128, bn, dtype, &p)) return err(FP_ERR_CUDA, refused);
+            if (!lay_out(prod + i, 1, 128, bn, bn, dtype, &p)) return err(FP_ERR_CUDA, refused);
             const int kblocks = p.prob[0].kblocks;
             int splits = 1;
             while (splits < 8 && p.tiles * splits * 2 <= sms && kblocks >= splits * 4) splits *= 2;
@@ -978,16 +1019,26 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, int* sta
                          : bn == 64 ? launch_tiles<64>(p, splits, smem, st) : launch_tiles<128>(p, splits, smem, st));
         } else if (tiles[i] > sms / 2) {
             static std::atomic<unsigned long long> done;
-            if (!lay_out(prod + i, 1, 256, 256, dtype, &p)) return err(FP_ERR_CUDA, refused);
+            if (!lay_out(prod + i, 1, 256, 256, 128, dtype, &p)) return err(FP_ERR_CUDA, refused);
             const cudaError_t e = allow_smem(linear_pair_kernel, kPairSmem, &done);
             s = launched(e != cudaSuccess ? e : launch_clusters(linear_pair_kernel, p, 2 * (sms / 2), kPairThreads, kPairSmem, 2, st));
         } else {
-            if (!lay_out(prod + i, 1, 256, 256, dtype, &p)) return err(FP_ERR_CUDA, refused);
-            // as many pairs a tile as its share of the SMs has room for, four K blocks a pair at least
-            const int kblocks = p.prob[0].kblocks, share = n > 1 && !few ? (int)(sms * tiles[i] * kblocks / work) : sms;
-            int S = kMaxSplits;
-            while (S > 1 && (2 * p.tiles * S > std::min(share, split_room(S)) || kblocks < 4 * S)) --S;
-            s = launched(S == 1 ? launch_split<1>(p, st) : S == 2 ? launch_split<2>(p, st) : S == 3 ? launch_split<3>(p, st) : launch_split<4>(p, st));
+            // The tile's width and the pairs that share it by the cycles that they are expected to take: the K blocks, the exchange of
+            // sums, finishing, and 3000 for everything else; a launch of more CTAs than run at once takes as many rounds.  Of
+            // two products each has its share of the SMs.
+            const int64_t kblocks = (prod[i].Kc + kBlockK - 1) / kBlockK;
+            const int64_t share = n > 1 && !few ? std::max<int64_t>(2, sms * tiles[i] * kblocks / work) : sms;
+            int bn = 256, S = 1;
+            double best = 0;
+            for (int b = 256; b >= 128; b /= 2)
+                for (int c = 1; c <= kMaxSplits && 2 * c <= std::max<int64_t>(kblocks, 2); ++c) {
+                    const int64_t ctas = 2 * c * ((prod[i].I + 255) / 256) * ((prod[i].J + b - 1) / b), room = std::min<int64_t>(share, split_room(c));
+                    const double cost = (double)((ctas + room - 1) / room) *
+                                        (3000 + (double)((kblocks + c - 1) / c) * (b == 256 ? 522 : 392) + 32.0 * b * (c - 1) / c + 11.0 * b / c);
+                    if (best == 0 || cost < best) { best = cost; bn = b; S = c; }
+                }
+            if (!lay_out(prod + i, 1, 256, bn, bn / 2, dtype, &p)) return err(FP_ERR_CUDA, refused);
+            s = launched(bn == 256 ? launch_split<256>(p, S, st) : launch_split<128>(p, S, st));
         }
         if (s != FP_OK) return s;
     }
