@@ -327,21 +327,21 @@ def _dtypes():
     return _dtype_codes
 
 
-def _dtype(t, name, want=None):
+def _dtype(t, name):
     code = _dtypes().get(t.dtype)
-    if code is None or (want is not None and code not in want):
+    if code is None:
         raise ValueError(f"{name} has dtype {t.dtype}")
     return code
 
 
-def _matrix(t, rows, cols, name, dtype=None):
-    """(address, row stride) of a rows x cols tensor whose rows are contiguous; (0, 0) of None."""
+def _matrix(t, shape, name, dtype=None):
+    """(address, row stride) of a tensor of that shape whose rows are contiguous; (0, 0) of None."""
     if t is None:
         return 0, 0
-    if t.shape != (rows, cols) or not t.is_cuda or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype} on {t.device}: a CUDA tensor of {(rows, cols)}, {dtype} is wanted")
+    if t.shape != shape or not t.is_cuda or (dtype is not None and t.dtype is not dtype):
+        raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype} on {t.device}: a CUDA tensor of {shape}, {dtype} is wanted")
     ld, step = t.stride()
-    if step != 1 and cols > 1:
+    if step != 1 and shape[1] > 1:
         raise ValueError(f"{name}: neighbours of a row must be neighbours in memory (strides {t.stride()})")
     return t.data_ptr(), ld
 
@@ -350,7 +350,7 @@ def _vector(t, n, name, dtype=None):
     """Address of a contiguous vector of n elements; 0 of None."""
     if t is None:
         return 0
-    if t.shape != (n,) or not t.is_cuda or (dtype is not None and t.dtype != dtype) or (n > 1 and t.stride(0) != 1):
+    if t.shape != (n,) or not t.is_cuda or (dtype is not None and t.dtype is not dtype) or (n > 1 and t.stride() != (1,)):
         raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype} on {t.device}: a contiguous CUDA vector of {n}, {dtype} is wanted")
     return t.data_ptr()
 
@@ -361,11 +361,12 @@ def _scratch(work):
 
 def _linear_values(x, w, y, bias, res, pre, act, res_first):
     (M, K), N, dt = x.shape, w.shape[0], x.dtype
-    px, lx = _matrix(x, M, K, "x")
-    pw, lw = _matrix(w, N, K, "w", dt)
-    py, ly = _matrix(y, M, N, "y")
-    pr, lr = _matrix(res, M, N, "res", dt)
-    pp, lp = _matrix(pre, M, N, "pre", dt)
+    out = (M, N)
+    px, lx = _matrix(x, (M, K), "x")
+    pw, lw = _matrix(w, (N, K), "w", dt)
+    py, ly = _matrix(y, out, "y")
+    pr, lr = _matrix(res, out, "res", dt) if res is not None else (0, 0)
+    pp, lp = _matrix(pre, out, "pre", dt) if pre is not None else (0, 0)
     return (M, N, K, _dtype(x, "x"), _dtype(y, "y"), 0 if bias is None else _dtype(bias, "bias"), act, 1 if res_first else 0, 0,
             px, pw, _vector(bias, N, "bias"), pr, py, pp, lx, lw, lr, ly, lp)
 
@@ -392,14 +393,14 @@ def fp_linear_workspace(x, w, y, bias=None, res=None, pre=None, act=FP_ACT_NONE,
 
 def _linear_grad_values(dy, x, w, dx, dw, db, dz, pre, act, accumulate):
     M, N = dy.shape
-    K, dt = next((t.shape[1] for t in (x, w, dx, dw) if t is not None), 1), dy.dtype
-    pdy, ldy = _matrix(dy, M, N, "dy")
-    px, lx = _matrix(x, M, K, "x", dt)
-    pw, lw = _matrix(w, N, K, "w", dt)
-    pdx, ldx = _matrix(dx, M, K, "dx", dt)
-    pdw, ldw = _matrix(dw, N, K, "dw")
-    pdz, ldz = _matrix(dz, M, N, "dz", dt)
-    pp, lp = _matrix(pre, M, N, "pre", dt)
+    K, dt, dy_shape = next((t.shape[1] for t in (x, w, dx, dw) if t is not None), 1), dy.dtype, (M, N)
+    pdy, ldy = _matrix(dy, dy_shape, "dy")
+    px, lx = _matrix(x, (M, K), "x", dt)
+    pw, lw = _matrix(w, (N, K), "w", dt)
+    pdx, ldx = _matrix(dx, (M, K), "dx", dt)
+    pdw, ldw = _matrix(dw, (N, K), "dw")
+    pdz, ldz = _matrix(dz, dy_shape, "dz", dt)
+    pp, lp = _matrix(pre, dy_shape, "pre", dt)
     out = dw if dw is not None else db
     code = _dtype(out, "dw") if out is not None else _dtype(dy, "dy")
     return (M, N, K, _dtype(dy, "dy"), code, act, 1 if accumulate else 0, pdy, pp, px, pw, pdx, pdw,
@@ -437,8 +438,8 @@ def fp_cross_entropy(logits, labels, loss=None, dlogits=None, row_grad=None, lab
     """Softmax cross-entropy of every row of logits (rows, classes) with int32 or int64 labels (rows): loss (rows, float32) and dlogits
     = grad_scale * row_grad * d loss / d logits, of the logits' type (it may be the logits themselves); either may be None."""
     rows, classes = logits.shape
-    px, lx = _matrix(logits, rows, classes, "logits")
-    pd, ld = _matrix(dlogits, rows, classes, "dlogits", logits.dtype)
+    px, lx = _matrix(logits, (rows, classes), "logits")
+    pd, ld = _matrix(dlogits, (rows, classes), "dlogits", logits.dtype)
     torch_f32, label_bytes = _f32_and_labels()
     size = label_bytes.get(labels.dtype)
     if size is None:
