@@ -259,7 +259,7 @@ __device__ __forceinline__ float largest_of_half(float x) {
 }
 
 template <int PT, int GT, int N>
-__global__ void __launch_bounds__(kThreads) adamw8_kernel(const __grid_constant__ Table<N> t) {
+__global__ void __launch_bounds__(kThreads, 4) adamw8_kernel(const __grid_constant__ Table<N> t) {
     const Entry& e = find(t, (int)blockIdx.x);
     const Step s = step_of(t.s);
     const int lane16 = threadIdx.x & 15;
