@@ -9,9 +9,10 @@
 // another's arithmetic.  Units lie at 16-byte boundaries of memory, whatever the row starts at: its first and last
 // one may be partial.  Where the gradient's row lies otherwise than the logits', a warp passes it through shared memory and writes
 // elements, neighbours by neighbouring lanes.  Rows longer than 32768 units are read twice.
-// Two exponentials and some ten instructions an element are close to what the memory leaves time for, hence: the maximum of 16-bit logits is
-// taken two at a time, what is missing of a partial unit counts as -inf instead of being asked for everywhere, and the label's own
-// element is written a second time instead of every element being compared with it.
+// Two exponentials and some ten instructions an element are close to what the memory leaves time for (with 23, 8192 x 32000 logits of 16 bits took
+// 210 us), hence: the maximum of 16-bit logits is taken two at a time, an exponential's argument is one fused product and sum, what is missing of
+// a partial unit counts as -inf instead of being asked for everywhere, and the label's own element is written a second time
+// instead of every element being compared with it.
 #include "train_common.cuh"
 #include "tc_common.cuh"
 
@@ -34,13 +35,27 @@ struct LossParams {
     float smoothing, scale;
 };
 
-// 2^x; results below 2^-126 are 0.  e^d as 2^(d log2 e): d = x - m is exact or rounded once, so large logits cost nothing.
+// 2^x; results below 2^-126 are 0.
 __device__ __forceinline__ float exp2_of(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float exp_of(float d) { return exp2_of(d * 1.4426950408889634f); }
+constexpr float kLog2E = 1.4426950408889634f;
+__device__ __forceinline__ float exp_of(float d) { return exp2_of(d * kLog2E); }
+// e^(x - m) as 2^(x log2e - c) `fix`: c = m log2e rounded, and 2^(c - m log2e), which a fused product and sum gives exactly, makes up for
+// the rounding, however large m is.  Only where c might overflow (`far`) the difference is taken first.
+struct Below {
+    float m, c, fix;
+    bool far;
+    __device__ __forceinline__ explicit Below(float m_) : m(m_) {
+        far = !(fabsf(m) < 1e37f);
+        c = m * kLog2E;
+        fix = far ? 1.0f : exp2_of(-fmaf(m, kLog2E, -c));
+    }
+    __device__ __forceinline__ float near_value(float x) const { return exp2_of(fmaf(x, kLog2E, -c)); }     // without fix
+    __device__ __forceinline__ float value(float x) const { return far ? exp_of(x - m) : near_value(x) * fix; }
+};
 
 // Maximum, sum of exponentials below it, and plain sum of a part of a row.  A part of -inf alone has m = -inf, s = 0.
 struct Part { float m, s, t; };
@@ -107,12 +122,21 @@ __device__ __forceinline__ Part part_of(const uint4 (&u)[V], int used) {
     Part a = {-INFINITY, 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < U::E; ++i) a.m = fmaxf(a.m, U::get(top, i));
-    const float m = a.m == -INFINITY ? 0.0f : a.m;       // (of -inf alone every exponential below is 0)
+    const Below e(a.m == -INFINITY ? 0.0f : a.m);        // (of -inf alone every exponential below is 0)
+    if (e.far) {
+#pragma unroll 1
+        for (int i = 0; i < U::E; ++i)
 #pragma unroll
-    for (int k = 0; k < V; ++k)
-        if (k < used)
+            for (int k = 0; k < V; ++k)
+                if (k < used) a.s += e.value(U::get(u[k], i));
+    } else {
 #pragma unroll
-            for (int i = 0; i < U::E; ++i) a.s += exp_of(U::get(u[k], i) - m);
+        for (int k = 0; k < V; ++k)
+            if (k < used)
+#pragma unroll
+                for (int i = 0; i < U::E; ++i) a.s += e.near_value(U::get(u[k], i));
+        a.s *= e.fix;
+    }
     return a;
 }
 
@@ -170,15 +194,17 @@ __device__ __forceinline__ float loss_of(const LossParams& p, const Row& r, cons
     return r.ignored ? 0.0f : r.bad ? NAN : l;
 }
 
-// The gradient's element from x: what is common to a row is in here.
+// The gradient's element from x, scale e^(x - m) - off: what is common to a row is in here.
 struct Slope {
-    float m, scale, off;                                 // scale (e^(x - m)) - off
-    __device__ __forceinline__ Slope(const LossParams& p, const Row& r, const Part& a) {
-        m = a.m;
+    Below e;
+    float scale, near_scale, off;
+    __device__ __forceinline__ Slope(const LossParams& p, const Row& r, const Part& a) : e(a.m) {
         scale = r.bad ? NAN : r.g / a.s;
+        near_scale = scale * e.fix;
         off = r.g * (p.smoothing / (float)p.C);
     }
-    __device__ __forceinline__ float operator()(float x) const { return fmaf(exp_of(x - m), scale, -off); }
+    __device__ __forceinline__ float near_value(float x) const { return fmaf(e.near_value(x), near_scale, -off); }
+    __device__ __forceinline__ float operator()(float x) const { return e.far ? fmaf(exp_of(x - e.m), scale, -off) : near_value(x); }
 };
 
 // Rows in registers: V units a thread, G threads a row (G < 256: several rows a block of 256), CL blocks.
@@ -238,9 +264,15 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, G < 512 ? 4 : 2) cross_entr
         for (int k = 0; k < V; ++k) {
             if (k >= used) break;
             const int n = t + k * kStep;
-            float v[8];
+            float v[8] = {};
+            if (slope.e.far) {
+                if (!r.ignored)
 #pragma unroll
-            for (int i = 0; i < E; ++i) v[i] = r.ignored ? 0.0f : slope(U::get(u[k], i));
+                    for (int i = 0; i < E; ++i) v[i] = slope(U::get(u[k], i));
+            } else if (!r.ignored) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) v[i] = slope.near_value(U::get(u[k], i));
+            }
             if (alike || G < 32) {
                 if (alike && n < units && full(n)) U::store(p.dx, to + (long long)n * E - shift, U::make(v));
                 else if (n < units)
