@@ -4,15 +4,16 @@
 // d loss / dx_j = exp(x_j - m) / s - e / C - (1 - e) [j = y].
 //
 // Memory bound: logits are read once and the gradient written once.  The gradient needs s, so a row has to be kept between the
-// two: in registers, up to eight 16-byte units a thread, by as many threads as that takes: 8, 32 .. 512, or 2, 4 or 8 blocks of
-// 512 as a cluster, whose maxima and sums meet in shared memory; more, smaller blocks an SM let one row's copies run beside
-// another's arithmetic.  Units lie at 16-byte boundaries of memory, whatever the row starts at: its first and last
-// one may be partial.  Where the gradient's row lies otherwise than the logits', a warp passes it through shared memory and writes
-// elements, neighbours by neighbouring lanes.  Rows longer than 32768 units are read twice.
-// Two exponentials and some ten instructions an element are close to what the memory leaves time for (with 23, 8192 x 32000 logits of 16 bits took
-// 210 us), hence: the maximum of 16-bit logits is taken two at a time, an exponential's argument is one fused product and sum, what is missing of
-// a partial unit counts as -inf instead of being asked for everywhere, and the label's own element is written a second time
-// instead of every element being compared with it.
+// two.  Rows of up to 1024 16-byte units stay in the registers of 8, 32 or 256 threads; longer ones in the shared memory of blocks
+// of 512, each thread's units in places that it alone reads, so that nothing waits for another thread's copies: up to nine units a thread, 72 KB, leave room for
+// three blocks on an SM, and one row's copies run beside another's arithmetic (in registers two blocks fit: 8192 x 32000 logits of 16 bits 212 us).
+// A row may be shared by 2, 4 or 8 blocks, a cluster, whose maxima and sums meet in shared memory.  Units lie at
+// 16-byte boundaries of memory, whatever the row starts at: its first and last one may be partial.  Where the gradient's row lies
+// otherwise than the logits', a warp passes it through shared memory and writes elements, neighbours by neighbouring lanes.  Rows of more than 110000 units are
+// read twice.
+// Two exponentials and some ten instructions an element are close to what the memory leaves time for, hence: the maximum of 16-bit logits is
+// taken two at a time, an exponential's argument is one fused product and sum, what is missing of a partial unit counts as -inf instead
+// of being asked for everywhere, and the label's own element is written a second time instead of every element being compared with it.
 #include "train_common.cuh"
 #include "tc_common.cuh"
 
@@ -207,16 +208,16 @@ struct Slope {
     __device__ __forceinline__ float operator()(float x) const { return e.far ? fmaf(exp_of(x - e.m), scale, -off) : near_value(x); }
 };
 
-// Rows in registers: V units a thread, G threads a row (G < 256: several rows a block of 256), CL blocks.
-template <int DT, int G, int V, int CL>
-__global__ void __launch_bounds__(G < 256 ? 256 : G, G < 512 ? 4 : 2) cross_entropy_kernel(const LossParams p) {
+// Rows in registers: V units a thread, G threads a row (G < 256: several rows a block of 256).
+template <int DT, int G, int V>
+__global__ void __launch_bounds__(256, 4) cross_entropy_kernel(const LossParams p) {
     typedef Unit<DT> U;
-    constexpr int E = U::E, B = G < 256 ? 256 : G, kStep = G * CL;
+    constexpr int E = U::E, kStep = G;
     __shared__ Part shared[33];
-    __shared__ uint4 staged[G < 32 ? 1 : B];
-    const long long row = CL > 1 ? (long long)(blockIdx.x / CL) : (long long)blockIdx.x * (B / G) + threadIdx.x / G;
+    __shared__ uint4 staged[G < 32 ? 1 : 256];
+    const long long row = (long long)blockIdx.x * (256 / G) + threadIdx.x / G;
     const bool there = row < p.rows;                     // (all threads of a row agree, and of a block of one row)
-    const int t = (CL > 1 ? (int)(blockIdx.x % CL) * G : 0) + (int)threadIdx.x % G, lane = threadIdx.x & 31;
+    const int t = (int)threadIdx.x % G, lane = threadIdx.x & 31;
     const long long at = row * p.ld_x, to = row * p.ld_dx;
     // unit n has elements n E - shift .. of the row; the first and the last may reach over its ends
     const int shift = U::shift(p.x, at), units = there ? (p.C + shift + E - 1) / E : 0, used = (units + kStep - 1) / kStep;
@@ -253,7 +254,7 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, G < 512 ? 4 : 2) cross_entr
 #pragma unroll
                 for (int i = 0; i < E; ++i)
                     if ((unsigned)((t + k * kStep) * E - shift + i) < (unsigned)p.C) a.t += U::get(u[k], i);
-    a = join_all<G, CL>(a, shared);
+    a = join_all<G, 1>(a, shared);
     if (there && p.loss && t == 0) p.loss[row] = loss_of(p, r, a);
     if (there && p.dx) {
         const Slope slope(p, r, a);
@@ -297,6 +298,136 @@ __global__ void __launch_bounds__(G < 256 ? 256 : G, G < 512 ? 4 : 2) cross_entr
         }
         if ((alike || G < 32) && labelled && (int)((r.label + shift) / E) % kStep == t)      // the thread that has just written it
             store1(p.dx, to + r.label, DT, own);
+    }
+}
+
+// Rows in shared memory: CL blocks of 512 threads.
+template <int DT, int CL>
+__global__ void __launch_bounds__(512, 3) cross_entropy_kept_kernel(const LossParams p) {
+    typedef Unit<DT> U;
+    constexpr int E = U::E, G = 512, kStep = G * CL;
+    extern __shared__ uint4 kept[];                      // unit t + k kStep of the row at kept[k G + thread]
+    __shared__ Part shared[33];
+    const long long row = (long long)(blockIdx.x / CL);
+    const int t = (int)(blockIdx.x % CL) * G + (int)threadIdx.x, lane = threadIdx.x & 31;
+    const long long at = row * p.ld_x, to = row * p.ld_dx;
+    const int shift = U::shift(p.x, at), units = (p.C + shift + E - 1) / E, used = (units + kStep - 1) / kStep;
+    auto full = [&](int n) { return n * E >= shift && n * E - shift + E <= p.C; };
+    uint4* const mine = kept + threadIdx.x;
+    // this thread's units: k = 0 .. count - 1, of which lo .. hi - 1 are whole (only the row's first and last may not be)
+    const int count = t < units ? (units - 1 - t) / kStep + 1 : 0;
+    const int lo = t == 0 && !full(0) ? 1 : 0, hi = count > lo && !full(t + (count - 1) * kStep) ? count - 1 : max(count, lo);
+    {
+        const char* src = static_cast<const char*>(p.x) + (at - shift) * (16 / E) + (long long)(t + lo * kStep) * 16;
+        uint32_t dst = tc::smem_u32(mine + lo * G);
+#pragma unroll 4
+        for (int k = lo; k < hi; ++k) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+            src += kStep * 16;
+            dst += G * 16;
+        }
+    }
+    auto partial = [&](int k) {
+        const int n = t + k * kStep;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < E && (unsigned)(n * E - shift + i) < (unsigned)p.C ? load1(p.x, at + n * E - shift + i, DT) : -INFINITY;
+        mine[k * G] = U::make(v);
+    };
+    if (lo) partial(0);
+    if (hi < count) partial(hi);
+    const Row r = row_of<DT>(p, row);
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    Part a = {-INFINITY, 0.0f, 0.0f};
+    {
+        uint4 top = U::nothing();
+#pragma unroll 4
+        for (int k = 0; k < count; ++k) top = U::larger(top, mine[k * G]);
+#pragma unroll
+        for (int i = 0; i < E; ++i) a.m = fmaxf(a.m, U::get(top, i));
+        const Below e(a.m == -INFINITY ? 0.0f : a.m);
+        if (e.far) {
+#pragma unroll 1
+            for (int k = 0; k < count; ++k) {
+                const uint4 u = mine[k * G];
+#pragma unroll
+                for (int i = 0; i < E; ++i) a.s += e.value(U::get(u, i));
+            }
+        } else {
+            float s[2] = {0.0f, 0.0f};
+#pragma unroll 4
+            for (int k = 0; k < count; ++k) {
+                const uint4 u = mine[k * G];
+#pragma unroll
+                for (int i = 0; i < E; ++i) s[i & 1] += e.near_value(U::get(u, i));
+            }
+            a.s = (s[0] + s[1]) * e.fix;
+        }
+    }
+    if (p.smoothing != 0.0f)
+#pragma unroll 1
+        for (int k = 0; k < count; ++k) {
+            const uint4 u = mine[k * G];
+            const bool whole = k >= lo && k < hi;
+#pragma unroll
+            for (int i = 0; i < E; ++i)
+                if (whole || (unsigned)((t + k * kStep) * E - shift + i) < (unsigned)p.C) a.t += U::get(u, i);
+        }
+    a = join_all<G, CL>(a, shared);                      // (and all have read what dx may overwrite)
+    if (p.loss && t == 0) p.loss[row] = loss_of(p, r, a);
+    if (p.dx) {
+        const Slope slope(p, r, a);
+        const float own = slope(r.label_x) - r.g * (1.0f - p.smoothing);         // the label's element
+        const bool labelled = !r.ignored && !r.bad, alike = U::shift(p.dx, to) == shift, plain = !r.ignored && !slope.e.far;
+        auto gradient = [&](const uint4& u) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] = r.ignored ? 0.0f : slope(U::get(u, i));
+            return U::make(v);
+        };
+        char* dst = static_cast<char*>(p.dx) + (to - shift) * (16 / E) + (long long)(t + lo * kStep) * 16;
+        if (alike && plain) {
+#pragma unroll 4
+            for (int k = lo; k < hi; ++k) {
+                const uint4 u = mine[k * G];
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < E; ++i) v[i] = slope.near_value(U::get(u, i));
+                __stcs(reinterpret_cast<uint4*>(dst), U::make(v));
+                dst += kStep * 16;
+            }
+        } else if (alike) {
+#pragma unroll 1
+            for (int k = lo; k < hi; ++k, dst += kStep * 16) __stcs(reinterpret_cast<uint4*>(dst), gradient(mine[k * G]));
+        }
+        if (alike) {
+            auto edge = [&](int k) {
+                const uint4 u = gradient(mine[k * G]);
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    const int j = (t + k * kStep) * E - shift + i;
+                    if ((unsigned)j < (unsigned)p.C) store1(p.dx, to + j, DT, U::get(u, i));
+                }
+            };
+            if (lo) edge(0);
+            if (hi < count) edge(hi);
+            if (labelled && (int)((r.label + shift) / E) % kStep == t) store1(p.dx, to + r.label, DT, own);      // the thread that has just written it
+        } else {                                         // through the units' own places
+            for (int k = 0; k < used; ++k) {
+                uint4* const warps = kept + k * G + (threadIdx.x & ~31u);
+                if (k < count) warps[lane] = gradient(mine[k * G]);
+                __syncwarp();
+                const int j0 = (t - lane + k * kStep) * E - shift;
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    const int j = j0 + 32 * i + lane;
+                    if ((unsigned)j >= (unsigned)p.C) continue;
+                    if (j == r.label && labelled) store1(p.dx, to + j, DT, own);
+                    else if (DT == FP_DTYPE_F32) static_cast<float*>(p.dx)[to + j] = reinterpret_cast<const float*>(warps)[32 * i + lane];
+                    else static_cast<uint16_t*>(p.dx)[to + j] = reinterpret_cast<const uint16_t*>(warps)[32 * i + lane];
+                }
+            }
+        }
     }
     if (CL > 1) tc::cluster_sync_all();                  // no block leaves while another may still read its part
 }
@@ -347,23 +478,24 @@ __global__ void __launch_bounds__(1024) cross_entropy_twice_kernel(const LossPar
 }
 
 typedef void (*Kernel)(const LossParams);
-struct Choice { Kernel k; int threads, rows_a_block, cluster; };
+struct Choice { Kernel k; int threads, rows_a_block, cluster, smem; };
 
-// The fewest threads that hold a row; for few long rows as many blocks as that spreads it over.
+constexpr int kMostUnits = 27;                           // a thread's units in shared memory: 216 KB a block
 template <int DT>
 Choice choose(long long C, long long rows) {
     const int sms = sm_count();
     const long long units = (C - 1) / Unit<DT>::E + 2;   // at the worst alignment
-    if (units <= 8 * 4) return {cross_entropy_kernel<DT, 8, 4, 1>, 256, 32, 1};
-    if (units <= 32 * 4) return {cross_entropy_kernel<DT, 32, 4, 1>, 256, 8, 1};
-    if (units <= 32 * 8 && rows > 8 * sms) return {cross_entropy_kernel<DT, 32, 8, 1>, 256, 8, 1};
-    if (units <= 256 * 4) return {cross_entropy_kernel<DT, 256, 4, 1>, 256, 1, 1};
-    if (units <= 512 * 8 && rows * 8 > sms) return {cross_entropy_kernel<DT, 512, 8, 1>, 512, 1, 1};
-    if (units <= 512 * 8 * 2 && rows * 8 > sms) return {cross_entropy_kernel<DT, 512, 8, 2>, 512, 1, 2};
-    if (units <= 512 * 8 * 4 && rows * 8 > sms) return {cross_entropy_kernel<DT, 512, 8, 4>, 512, 1, 4};
-    if (units <= 512 * 4 * 8) return {cross_entropy_kernel<DT, 512, 4, 8>, 512, 1, 8};
-    if (units <= 512 * 8 * 8) return {cross_entropy_kernel<DT, 512, 8, 8>, 512, 1, 8};
-    return {cross_entropy_twice_kernel<DT, 8>, 1024, 1, 8};
+    if (units <= 8 * 4) return {cross_entropy_kernel<DT, 8, 4>, 256, 32, 1, 0};
+    if (units <= 32 * 4) return {cross_entropy_kernel<DT, 32, 4>, 256, 8, 1, 0};
+    if (units <= 32 * 8 && rows > 8 * sms) return {cross_entropy_kernel<DT, 32, 8>, 256, 8, 1, 0};
+    if (units <= 256 * 4) return {cross_entropy_kernel<DT, 256, 4>, 256, 1, 1, 0};
+    // as few blocks a row as leave three on an SM; more where there are few rows
+    int cl = 1;
+    while (cl < 8 && ((units + 512 * cl - 1) / (512 * cl) > 9 || (rows * cl * 2 <= sms && units > 512 * cl))) cl *= 2;
+    const long long each = (units + 512 * cl - 1) / (512 * cl);
+    if (each > kMostUnits) return {cross_entropy_twice_kernel<DT, 8>, 1024, 1, 8, 0};
+    return {cl == 1 ? cross_entropy_kept_kernel<DT, 1> : cl == 2 ? cross_entropy_kept_kernel<DT, 2> : cl == 4 ? cross_entropy_kept_kernel<DT, 4>
+                                                                                             : cross_entropy_kept_kernel<DT, 8>, 512, 1, cl, (int)each * 512 * 16};
 }
 
 }  // namespace
@@ -408,7 +540,12 @@ extern "C" fp_status fp_cross_entropy(const fp_cross_entropy_args* a, void* stre
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3((unsigned)c.threads);
+    cfg.dynamicSmemBytes = (size_t)c.smem;
     cfg.stream = (cudaStream_t)stream;
+    if (c.smem > 48 * 1024 && cudaFuncSetAttribute((const void*)c.k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostUnits * 512 * 16) != cudaSuccess) {
+        cudaGetLastError();
+        return err(FP_ERR_CUDA, "fp_cross_entropy: no room for a row in shared memory");
+    }
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = (unsigned)c.cluster;
