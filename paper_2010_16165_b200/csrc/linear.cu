@@ -26,9 +26,14 @@ using namespace train;
 
 constexpr int kBlockK = 64;                              // elements of the sum a stage: 128 bytes, a swizzled row
 constexpr int64_t kMaxSize = 1ll << 30;
-constexpr int kMaxSmem = 232448;                         // shared memory a block may have
+constexpr int kMaxSmem = 232448, kAllSmem = kMaxSmem - 512;      // shared memory a block may have, and without what these kernels have statically
 
 __device__ int g_linear_status;                          // raised by a bounded wait that ran out
+
+// The tensor cores cut a sum's low bits at every step instead of rounding, always toward zero: after 1024 terms 32-bit sums are 1e-6 too small, after
+// 16384 2e-5 (measured; with terms of random signs).  Results in 16 bits do not show it; where a result is written in 32 bits, a sum is
+// taken in runs of at most kRun K blocks (where there is room for that many), which are added by rounded additions.
+constexpr int kRun = 8;
 
 // What is done with a finished sum.  Outputs are rows of n neighbours; the accumulator has n along j, or with `swap` along i.
 struct Epilogue {
@@ -50,6 +55,7 @@ struct Problem {
 struct TileParams {
     Problem prob[2];
     int n_prob, stages, tiles;
+    int run;                                             // K blocks that an accumulator adds up before another one takes over (see kRun)
     int late;                                            // this launch's operands were there before the launch in front of it began: see after_the_last()
     uint32_t bf16;
     int* status;
@@ -67,14 +73,18 @@ __device__ __forceinline__ bool mbar_poll(uint32_t bar, uint32_t parity, volatil
         if (*abort_flag || clock64() - t0 > limit_cycles) return false;
     }
 }
-// Launches of these kernels overlap: each may begin while the one before it ends, prepares its barriers and tensor memory, and then
-// waits here for that one's results.  It lets the next one begin after that wait, so when the next one runs, all that was complete
-// before THIS launch is; a product that needs no more (the second of a call) is `late`: it waits only before it ends, so
-// that whatever follows it still follows both.
+// Launches of these kernels overlap: each may begin while the one before it ends, prepares its barriers, and then waits here for
+// that one's results.  It lets the next one begin after that wait, so when the next one runs, all that was complete before
+// THIS launch is; a product that needs no more (the second of a call) is `late`: it waits only before it ends, so that whatever
+// follows it still follows both.
+// Tensor memory: an allocation blocks while other CTAs of the SM hold the columns, so a CTA that holds some must never wait for one that may be
+// blocked.  Hence it is taken after the wait for the launch before, and before the next launch may begin; and the CTAs of a
+// cluster, which wait for each other, take an SM's whole shared memory (kAllSmem), so that no other CTA with tensor memory, of this stream or of
+// another, is on their SMs.
 __device__ __forceinline__ void after_the_last(int late) {
     if (!late) asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
+__device__ __forceinline__ void let_the_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void before_the_end(int late) {
     if (late) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
@@ -237,13 +247,16 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     extern __shared__ uint8_t smem_raw[];
     __shared__ TileCtrl ctrl;
     constexpr uint32_t kStage = 128 * 128 + BN * 128;
-    constexpr int kCols = BN < 32 ? 32 : BN;
+    constexpr int kMost = 512 / BN < 16 ? 512 / BN : 16;             // accumulators at most
+    const uint32_t cols = p.run ? (uint32_t)(kMost * BN) : BN < 32 ? 32u : (uint32_t)BN;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = S > 1 ? cluster_rank() : 0u;
     const Problem& q = p.prob[0];
     const int tile = (int)(blockIdx.x / (unsigned)S), i0 = tile * 128;
     const int kb0 = (int)((long long)q.kblocks * rank / S), kb1 = (int)((long long)q.kblocks * (rank + 1) / S);
+    // accumulators of this CTA's part of the sum: one, or one every `run` K blocks
+    const int run = p.run ? max(p.run, (kb1 - kb0 + kMost - 1) / kMost) : kb1 - kb0, sums = (kb1 - kb0 + run - 1) / run;
     volatile int* abort_flag = &ctrl.abort_flag;
     const uint32_t full0 = smem_u32(ctrl.full), empty0 = smem_u32(ctrl.empty), done = smem_u32(&ctrl.done);
 
@@ -256,15 +269,17 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
             ctrl.abort_flag = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
-    } else if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl.tmem)), "r"((uint32_t)kCols) : "memory");
+    }
+    after_the_last(p.late);
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl.tmem)), "r"(cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctrl.tmem;
-    after_the_last(p.late);
+    let_the_next_begin();
     bool ok = true;
     if (warp == 0) {
         int stage = 0;
@@ -291,14 +306,19 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
         const uint32_t idesc = f16_idesc((int)p.bf16, q.a_mn, 0, 128, BN), a_step = q.a_mn ? 128u : 2u;
         int stage = 0;
         uint32_t phase = 0;
+        uint32_t d = tmem;
+        int left = run;                                  // K blocks until the next accumulator
         for (int kb = kb0; kb < kb1; ++kb) {
             ok = __all_sync(0xffffffffu, mbar_poll(full0 + 8 * stage, phase, abort_flag));
             if (!ok) break;
             tc_fence_after();
+            bool begins = kb == kb0;
+            if (left == 0) { left = run; d += BN; begins = true; }
+            --left;
             const uint32_t a = base + (uint32_t)stage * kStage;
             const uint32_t al = sw128_lo(a, 8192), bl = sw128_lo(a + 128 * 128, 8192), leader = elect_one();
 #pragma unroll
-            for (int s = 0; s < 4; ++s) umma_sw128_if(leader, tmem, al + (uint32_t)s * a_step, bl + (uint32_t)s * 2u, idesc, kb > kb0 || s ? 1u : 0u);
+            for (int s = 0; s < 4; ++s) umma_sw128_if(leader, d, al + (uint32_t)s * a_step, bl + (uint32_t)s * 2u, idesc, !begins || s ? 1u : 0u);
             if (leader) {
                 umma_commit(empty0 + 8 * stage);
                 if (kb == kb1 - 1) umma_commit(done);
@@ -332,6 +352,14 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
             uint32_t v[8];
             tmem_ld8(taddr + (uint32_t)r, v);
             tmem_ld_wait();
+#pragma unroll 1
+            for (int x = 1; x < sums; ++x) {
+                uint32_t u[8];
+                tmem_ld8(taddr + (uint32_t)(x * BN + r), u);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(u[i]));
+            }
             const uint32_t to = base + (uint32_t)(r * kPitch + col) * 4u;
 #pragma unroll
             for (int i = 0; i < 8; ++i) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + (uint32_t)(i * kPitch) * 4u), "r"(v[i]) : "memory");
@@ -349,7 +377,7 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
     else __syncthreads();
     if (warp == 1) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)kCols) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
     }
     before_the_end(p.late);
 }
@@ -360,14 +388,17 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
 // each and reads 32 KB.  Pairs are persistent; accumulators of two tiles fill tensor memory, so that a tile is finished by eight
 // warps while the next one is summed.  Warp 0 copies, warp 1 of the pair's first CTA issues the MMAs, warps 4-11 finish.
 
-constexpr int kPairThreads = 384, kPairStages = 5;
+// With RUNS the accumulators hold runs of a tile's sum instead (see kRun): sixteen warps add them up in registers.
+
 constexpr uint32_t kPairStage = 2 * 128 * 128;           // bytes of a stage in each CTA: 128 rows of A, 128 of B
 constexpr uint32_t kEpiPitch = 36;                       // words; 16-byte accesses of neighbouring lanes in different banks
 constexpr uint32_t kEpiWarp = 32 * kEpiPitch * 4;
-constexpr int kPairSmem = kPairStages * (int)kPairStage + 8 * (int)kEpiWarp + 1024;
-
+template <bool RUNS> struct PairShape {
+    static constexpr int kWarps = RUNS ? 16 : 8, kThreads = 128 + 32 * kWarps, kStages = RUNS ? 4 : 5, kCols = 1024 / kWarps;      // warps that finish, and a warp's columns
+    static_assert(kStages * (int)kPairStage + kWarps * (int)kEpiWarp + 1024 <= kAllSmem, "");
+};
 struct PairCtrl {
-    uint64_t full[kPairStages], empty[kPairStages], sums_full[2], sums_empty[2];
+    uint64_t full[5], empty[5], sums_full[2], sums_empty[2];
     uint32_t tmem;
     int abort_flag;
 };
@@ -422,9 +453,12 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap& map, 
     }
 }
 
-__global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __grid_constant__ TileParams p) {
+template <bool RUNS>
+__global__ void __launch_bounds__(PairShape<RUNS>::kThreads, 1) linear_pair_kernel(const __grid_constant__ TileParams p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ PairCtrl ctrl;
+    typedef PairShape<RUNS> Shape;
+    constexpr int kStages = Shape::kStages, kCols = Shape::kCols;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank();
@@ -435,12 +469,14 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
     if (warp == 0) {
         if (lane == 0) {
             for (int i = 0; i < p.n_prob; ++i) { prefetch_map(&p.prob[i].a); prefetch_map(&p.prob[i].b); }
-            for (int s = 0; s < kPairStages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
-            for (int s = 0; s < 2; ++s) { mbar_init(sums_full + 8 * s, 1); mbar_init(sums_empty + 8 * s, 16); }
+            for (int s = 0; s < kStages; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
+            for (int s = 0; s < 2; ++s) { mbar_init(sums_full + 8 * s, 1); mbar_init(sums_empty + 8 * s, 2 * Shape::kWarps); }
             ctrl.abort_flag = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
-    } else if (warp == 1) {
+    }
+    after_the_last(p.late);
+    if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl.tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
@@ -448,7 +484,7 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = ctrl.tmem;
-    after_the_last(p.late);
+    let_the_next_begin();
     bool ok = true;
     if (warp == 0) {
         uint32_t stage = 0, phase = 0;
@@ -466,82 +502,119 @@ __global__ void __launch_bounds__(kPairThreads, 1) linear_pair_kernel(const __gr
                     load_rows<128>(a + 128 * 128, w.q->b, w.q->b_mn, j0, kb * kBlockK, bar);
                 }
                 __syncwarp();
-                if (++stage == kPairStages) { stage = 0; phase ^= 1u; again = true; }
+                if (++stage == kStages) { stage = 0; phase ^= 1u; again = true; }
             }
         }
     } else if (warp == 1 && rank == 0) {
         uint32_t stage = 0, phase = 0, n = 0;
-        for (int t = pair; t < p.tiles && ok; t += pairs, ++n) {
+        for (int t = pair; t < p.tiles && ok; t += pairs) {
             const Place w = pair_place<256>(p, t);
             const uint32_t idesc = f16_idesc((int)p.bf16, w.q->a_mn, w.q->b_mn, 256, 256);
-            const uint32_t a_step = w.q->a_mn ? 128u : 2u, b_step = w.q->b_mn ? 128u : 2u, d = tmem + (n & 1) * 256u;
-            if (n >= 2) ok = __all_sync(0xffffffffu, mbar_poll(sums_empty + 8 * (n & 1), ((n >> 1) & 1u) ^ 1u, abort_flag));
-            if (!ok) break;
-            tc_fence_after();
+            const uint32_t a_step = w.q->a_mn ? 128u : 2u, b_step = w.q->b_mn ? 128u : 2u;
+            uint32_t d = tmem;
+            int left = 0;                                // K blocks until the next accumulator
             for (int kb = 0; kb < w.q->kblocks; ++kb) {
+                const bool begins = RUNS ? left == 0 : kb == 0;
+                if (begins) {
+                    left = p.run;
+                    d = tmem + (n & 1) * 256u;
+                    if (n >= 2) ok = __all_sync(0xffffffffu, mbar_poll(sums_empty + 8 * (n & 1), ((n >> 1) & 1u) ^ 1u, abort_flag));
+                    if (!ok) break;
+                }
                 ok = __all_sync(0xffffffffu, mbar_poll(full0 + 8 * stage, phase, abort_flag));
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t a = base + stage * kPairStage, al = sw128_lo(a, 8192), bl = sw128_lo(a + 128 * 128, 8192), leader = elect_one();
 #pragma unroll
                 for (int s = 0; s < 4; ++s)
-                    umma_sw128_pair_if(leader, d, al + (uint32_t)s * a_step, bl + (uint32_t)s * b_step, idesc, kb || s ? 1u : 0u);
+                    umma_sw128_pair_if(leader, d, al + (uint32_t)s * a_step, bl + (uint32_t)s * b_step, idesc, !begins || s ? 1u : 0u);
+                const bool ends = kb == w.q->kblocks - 1 || (RUNS && --left == 0);
                 if (leader) {
                     umma_commit_pair(empty0 + 8 * stage, 0);
-                    if (kb == w.q->kblocks - 1) umma_commit_pair(sums_full + 8 * (n & 1), 0);
+                    if (ends) umma_commit_pair(sums_full + 8 * (n & 1), 0);
                 }
                 __syncwarp();
-                if (++stage == kPairStages) { stage = 0; phase ^= 1u; }
+                if (ends) ++n;
+                if (++stage == kStages) { stage = 0; phase ^= 1u; }
             }
         }
     } else if (warp >= 4) {
-        const int quarter = warp & 3, half = (warp - 4) >> 2;
-        const uint32_t buf = base + kPairStages * kPairStage + (uint32_t)(warp - 4) * kEpiWarp;
+        const int quarter = warp & 3, col_w = ((warp - 4) >> 2) * kCols;
+        const uint32_t buf = base + kStages * kPairStage + (uint32_t)(warp - 4) * kEpiWarp, taddr = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)col_w;
         const uint32_t put = buf + (uint32_t)lane * (kEpiPitch * 4), get = buf + (uint32_t)(lane >> 3) * (kEpiPitch * 4) + (uint32_t)(lane & 7) * 16u;
         uint32_t n = 0;
-        for (int t = pair; t < p.tiles; t += pairs, ++n) {
+        for (int t = pair; t < p.tiles && ok; t += pairs) {
             const Place w = pair_place<256>(p, t);
             const Epilogue e = held(w.q->e);
-            ok = __all_sync(0xffffffffu, mbar_poll(sums_full + 8 * (n & 1), (n >> 1) & 1u, abort_flag, sum_limit(w.q->kblocks)));
-            if (!ok) break;
-            tc_fence_after();
-            const int row0 = w.i0 + 128 * (int)rank + 32 * quarter;
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                uint32_t v[32];
-                tmem_ld32(tmem + ((uint32_t)(32 * quarter) << 16) + (n & 1) * 256u + (uint32_t)(half * 128 + 32 * c), v);
-                const int col0 = w.j0 + half * 128 + 32 * c;
-                tmem_ld_wait();
-                if (c == 3) {                            // the accumulator is free for the tile after the next
+            float sum[2][RUNS ? 32 : 1];                 // with RUNS: this lane's columns col_w .., 32 and 32
+            if (RUNS)
+#pragma unroll
+                for (int i = 0; i < 64; ++i) sum[i >> 5][RUNS ? i & 31 : 0] = 0.0f;
+            if (RUNS) {
+                for (int kb = 0; kb < w.q->kblocks; kb += p.run, ++n) {
+                    ok = __all_sync(0xffffffffu, mbar_poll(sums_full + 8 * (n & 1), (n >> 1) & 1u, abort_flag, sum_limit(p.run)));
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[16];
+                        tmem_ld16(taddr + (n & 1) * 256u + (uint32_t)(16 * c), v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[c >> 1][RUNS ? 16 * (c & 1) + i : 0] += __uint_as_float(v[i]);
+                    }
                     tc_fence_before();
                     if (lane == 0) mbar_arrive_cluster(cluster_addr(sums_empty + 8 * (n & 1), 0));
+                }
+            } else {
+                ok = __all_sync(0xffffffffu, mbar_poll(sums_full + 8 * (n & 1), (n >> 1) & 1u, abort_flag, sum_limit(w.q->kblocks)));
+                tc_fence_after();
+            }
+            if (!ok) break;
+            const int row0 = w.i0 + 128 * (int)rank + 32 * quarter;
+#pragma unroll 1
+            for (int c = 0; c < kCols / 32; ++c) {
+                uint32_t v[32];
+                const int col0 = w.j0 + col_w + 32 * c;
+                if (RUNS) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) { v[i] = __float_as_uint(sum[0][RUNS ? i : 0]); sum[0][RUNS ? i : 0] = sum[1][RUNS ? i : 0]; }
+                } else {
+                    tmem_ld32(taddr + (n & 1) * 256u + (uint32_t)(32 * c), v);
+                    tmem_ld_wait();
+                    if (c == kCols / 32 - 1) {           // the accumulator is free for the tile after the next
+                        tc_fence_before();
+                        if (lane == 0) mbar_arrive_cluster(cluster_addr(sums_empty + 8 * (n & 1), 0));
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(put + (uint32_t)i * 16u), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
                 __syncwarp();
                 if (e.vec) {                             // four rows at a time, eight lanes a row
-                    const int n = col0 + (lane & 7) * 4;
-                    if (n < w.q->J) {
+                    const int col = col0 + (lane & 7) * 4;
+                    if (col < w.q->J) {
                         float bias[4];
-                        bias4<true>(e, n, w.q->J, bias);
+                        bias4<true>(e, col, w.q->J, bias);
+                        constexpr int U = RUNS ? 1 : 4;
 #pragma unroll 1
-                        for (int r = 0; r < 8; r += 4) {
-                            float x[4][4], res[4][4];
-                            fetch<4, true>(e, row0 + (lane >> 3) + 4 * r, 4, w.q->I, n, w.q->J, res);
+                        for (int r = 0; r < 8; r += U) {
+                            float x[U][4], res[U][4];
+                            fetch<U, true>(e, row0 + (lane >> 3) + 4 * r, 4, w.q->I, col, w.q->J, res);
 #pragma unroll
-                            for (int u = 0; u < 4; ++u) lds4<true>(get + (uint32_t)(4 * (r + u)) * (kEpiPitch * 4), x[u]);
-                            finish<4, true>(e, row0 + (lane >> 3) + 4 * r, 4, w.q->I, n, w.q->J, x, bias, res);
+                            for (int u = 0; u < U; ++u) lds4<true>(get + (uint32_t)(4 * (r + u)) * (kEpiPitch * 4), x[u]);
+                            finish<U, true>(e, row0 + (lane >> 3) + 4 * r, 4, w.q->I, col, w.q->J, x, bias, res);
                         }
                     }
                 } else if (col0 + lane < w.q->J) {       // a lane a column, four rows in the places of four columns
-                    const int n = col0 + lane;
-                    const float bias = e.bias ? load1(e.bias, n, e.bias_type) : 0.0f;
+                    const int col = col0 + lane;
+                    const float bias = e.bias ? load1(e.bias, col, e.bias_type) : 0.0f;
 #pragma unroll 1
-                    for (int r = 0; r < 32; r += 8) finish_column(e, row0 + r, w.q->I, n, buf + (uint32_t)(r * kEpiPitch + lane) * 4u, bias);
+                    for (int r = 0; r < 32; r += 8) finish_column(e, row0 + r, w.q->I, col, buf + (uint32_t)(r * kEpiPitch + lane) * 4u, bias);
                 }
                 __syncwarp();
             }
+            if (!RUNS) ++n;
         }
     }
     if (!ok && lane == 0) { atomicExch(&ctrl.abort_flag, 1); atomicExch(p.status, 1); }
@@ -566,8 +639,7 @@ constexpr int kSplitThreads = 512;
 template <int BN> struct SplitShape {
     static constexpr int kStages = BN == 256 ? 5 : 7, kPitch = BN + 4;     // words of a row of sums: 16-byte accesses of neighbouring lanes in different banks
     static constexpr uint32_t kStage = 128 * 128 + BN / 2 * 128;
-    static constexpr int kSmem = kStages * (int)kStage + 1024;
-    static_assert(128 * kPitch * 4 <= kStages * (int)kStage, "the sums take the stages' memory");
+    static_assert(kStages * (int)kStage + 1024 <= kAllSmem && 128 * kPitch * 4 <= kStages * (int)kStage, "the sums take the stages' memory");
 };
 struct SplitCtrl {
     uint64_t full[8], empty[8], done;
@@ -590,6 +662,8 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
     const Problem& q = *w.q;
     const int i0 = w.i0 + 128 * (int)half;
     const int kb0 = (int)((long long)q.kblocks * split / S), kb1 = (int)((long long)q.kblocks * (split + 1) / S);
+    // accumulators of this CTA's part of the sum: one, or one every `run` K blocks, as many as tensor memory holds
+    const int run = p.run ? max(p.run, (kb1 - kb0 + 512 / BN - 1) / (512 / BN)) : kb1 - kb0, sums = (kb1 - kb0 + run - 1) / run;
     volatile int* abort_flag = &ctrl.abort_flag;
     const uint32_t full0 = smem_u32(ctrl.full), empty0 = smem_u32(ctrl.empty), done = smem_u32(&ctrl.done);
 
@@ -602,15 +676,17 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
             ctrl.abort_flag = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
-    } else if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl.tmem)), "r"((uint32_t)BN) : "memory");
+    }
+    after_the_last(p.late);
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl.tmem)), "r"(p.run ? 512u : (uint32_t)BN) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
     tc_fence_before();
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = ctrl.tmem;
-    after_the_last(p.late);
+    let_the_next_begin();
     bool ok = true;
     if (warp == 0) {
         uint32_t stage = 0, phase = 0;
@@ -630,14 +706,19 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
     } else if (warp == 1 && half == 0) {
         uint32_t stage = 0, phase = 0;
         const uint32_t idesc = f16_idesc((int)p.bf16, q.a_mn, q.b_mn, 256, BN), a_step = q.a_mn ? 128u : 2u, b_step = q.b_mn ? 128u : 2u;
+        uint32_t d = tmem;
+        int left = run;                                  // K blocks until the next accumulator
         for (int kb = kb0; kb < kb1; ++kb) {
             ok = __all_sync(0xffffffffu, mbar_poll(full0 + 8 * stage, phase, abort_flag));
             if (!ok) break;
             tc_fence_after();
+            bool begins = kb == kb0;
+            if (left == 0) { left = run; d += BN; begins = true; }
+            --left;
             const uint32_t a = base + stage * kStage, al = sw128_lo(a, 8192), bl = sw128_lo(a + 128 * 128, 8192), leader = elect_one();
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                umma_sw128_pair_if(leader, tmem, al + (uint32_t)s * a_step, bl + (uint32_t)s * b_step, idesc, kb > kb0 || s ? 1u : 0u);
+                umma_sw128_pair_if(leader, d, al + (uint32_t)s * a_step, bl + (uint32_t)s * b_step, idesc, !begins || s ? 1u : 0u);
             if (leader) {
                 umma_commit_pair(empty0 + 8 * stage, first);
                 if (kb == kb1 - 1) umma_commit_pair(done, first);
@@ -664,6 +745,14 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
             uint32_t v[32];
             tmem_ld32(taddr + (uint32_t)(32 * c), v);
             tmem_ld_wait();
+#pragma unroll 1
+            for (int x = 1; x < sums; ++x) {
+                uint32_t u[32];
+                tmem_ld32(taddr + (uint32_t)(x * BN + 32 * c), u);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(u[i]));
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (uint32_t)(32 * c + 4 * i) * 4u), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
@@ -686,7 +775,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
     cluster_sync_all();                                          // no CTA leaves while another may still read its sums or signal it
     if (warp == 1) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)BN) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(p.run ? 512u : (uint32_t)BN) : "memory");
     }
     before_the_end(p.late);
 }
@@ -706,6 +795,7 @@ struct CopyParams { CopyJob job[2]; long long warps; };
 // instruction: whatever the alignment the lines are used whole.
 __global__ void __launch_bounds__(256) copy_rows_kernel(const __grid_constant__ CopyParams p) {
     after_the_last(0);
+    let_the_next_begin();
     const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     if (w >= p.warps) return;
     const CopyJob& j = p.job[w >= p.job[1].warp0 ? 1 : 0];
@@ -740,6 +830,7 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzParams p) {
     __shared__ float part[16][128];
     __shared__ float sums[128];
     after_the_last(0);
+    let_the_next_begin();
     const int lane = threadIdx.x & 15, half = threadIdx.x >> 4;
     const int split = (int)(blockIdx.x % (unsigned)p.splits);
     const int n0 = (int)(blockIdx.x / (unsigned)p.splits) * 128;
@@ -927,7 +1018,7 @@ int split_room(int S);
 template <int BN, int S>
 cudaError_t launch_tiles_of(const TileParams& p, int smem, cudaStream_t st) {
     static std::atomic<unsigned long long> done;
-    const cudaError_t e = allow_smem(linear_tile_kernel<BN, S>, kMaxSmem - (int)sizeof(TileCtrl) - 64, &done);
+    const cudaError_t e = allow_smem(linear_tile_kernel<BN, S>, kAllSmem, &done);
     return e != cudaSuccess ? e : launch_clusters(linear_tile_kernel<BN, S>, p, p.tiles * S, kTileThreads, smem, S, st);
 }
 template <int BN>
@@ -938,8 +1029,8 @@ cudaError_t launch_tiles(const TileParams& p, int splits, int smem, cudaStream_t
 template <int BN, int S>
 cudaError_t launch_split_of(const TileParams& p, cudaStream_t st) {
     static std::atomic<unsigned long long> done;
-    const cudaError_t e = allow_smem(linear_split_kernel<BN, S>, SplitShape<BN>::kSmem, &done);
-    return e != cudaSuccess ? e : launch_clusters(linear_split_kernel<BN, S>, p, 2 * p.tiles * S, kSplitThreads, SplitShape<BN>::kSmem, 2 * S, st);
+    const cudaError_t e = allow_smem(linear_split_kernel<BN, S>, kAllSmem, &done);
+    return e != cudaSuccess ? e : launch_clusters(linear_split_kernel<BN, S>, p, 2 * p.tiles * S, kSplitThreads, kAllSmem, 2 * S, st);
 }
 template <int BN>
 cudaError_t launch_split(const TileParams& p, int S, cudaStream_t st) {
@@ -957,14 +1048,14 @@ int split_room(int S) {
         memset(&cfg, 0, sizeof(cfg));
         cfg.gridDim = dim3((unsigned)(2 * S * 512));
         cfg.blockDim = dim3(kSplitThreads);
-        cfg.dynamicSmemBytes = SplitShape<256>::kSmem;
+        cfg.dynamicSmemBytes = kAllSmem;
         cudaLaunchAttribute attr;
         attr.id = cudaLaunchAttributeClusterDimension;
         attr.val.clusterDim.x = (unsigned)(2 * S);
         attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
         cfg.attrs = &attr;
         cfg.numAttrs = 1;
-        if (cudaFuncSetAttribute(linear_split_kernel<256, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, SplitShape<256>::kSmem) != cudaSuccess ||
+        if (cudaFuncSetAttribute(linear_split_kernel<256, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAllSmem) != cudaSuccess ||
             cudaOccupancyMaxActiveClusters(&n, linear_split_kernel<256, 2>, &cfg) != cudaSuccess || n <= 0) {
             cudaGetLastError();
             n = 1;
@@ -995,33 +1086,41 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, int* sta
         tiles[i] = ((prod[i].I + 255) / 256) * ((prod[i].J + 255) / 256);
         work += tiles[i] * ((prod[i].Kc + kBlockK - 1) / kBlockK);
     }
+    auto wide = [&](int i) { return prod[i].e.y_type == FP_DTYPE_F32 && prod[i].Kc > (int64_t)kRun * kBlockK; };      // see kRun
+    auto pairs = [&](bool runs) -> cudaError_t {
+        static std::atomic<unsigned long long> done[2];
+        p.run = runs ? kRun : 0;
+        cudaError_t e = runs ? allow_smem(linear_pair_kernel<true>, kAllSmem, &done[1]) : allow_smem(linear_pair_kernel<false>, kAllSmem, &done[0]);
+        if (e != cudaSuccess) return e;
+        return runs ? launch_clusters(linear_pair_kernel<true>, p, 2 * (sms / 2), PairShape<true>::kThreads, kAllSmem, 2, st)
+                    : launch_clusters(linear_pair_kernel<false>, p, 2 * (sms / 2), PairShape<false>::kThreads, kAllSmem, 2, st);
+    };
     if (!few && tiles[0] + tiles[1] > sms / 2) {
-        static std::atomic<unsigned long long> done;
         if (!lay_out(prod, n, 256, 256, 128, dtype, &p)) return err(FP_ERR_CUDA, refused);
         p.late = late;
-        const cudaError_t e = allow_smem(linear_pair_kernel, kPairSmem, &done);
-        return launched(e != cudaSuccess ? e : launch_clusters(linear_pair_kernel, p, 2 * (sms / 2), kPairThreads, kPairSmem, 2, st));
+        return launched(pairs(wide(0) || (n > 1 && wide(1))));
     }
     // one after the other, the second beside the first
     for (int i = 0; i < n; ++i) {
         fp_status s;
         p.late = late || i > 0;
+        p.run = wide(i) ? kRun : 0;
         if (prod[i].swap) {
             const int bn = prod[i].J <= 16 ? 16 : prod[i].J <= 32 ? 32 : prod[i].J <= 64 ? 64 : 128;
             if (!lay_out(prod + i, 1, 128, bn, bn, dtype, &p)) return err(FP_ERR_CUDA, refused);
             const int kblocks = p.prob[0].kblocks;
             int splits = 1;
-            while (splits < 8 && p.tiles * splits * 2 <= sms && kblocks >= splits * 4) splits *= 2;
-            const int stage = 128 * 128 + bn * 128, room = p.tiles * splits > sms ? kMaxSmem / 2 - 3072 : kMaxSmem - 3072;
+            const int most = p.run ? std::min(512 / bn, 16) : 1;       // accumulators
+            while (splits < 8 && kblocks >= splits * 4 && (p.tiles * splits * 2 <= sms || (p.run && kblocks > 2 * kRun * most * splits))) splits *= 2;
+            // (two CTAs on an SM share its 512 columns)
+            const int stage = 128 * 128 + bn * 128, room = p.tiles * splits > sms && most * bn <= 256 ? kMaxSmem / 2 - 3072 : kMaxSmem - 3072;
             p.stages = std::min(std::min(room / stage, 16), (kblocks + splits - 1) / splits);
-            const int smem = std::max(p.stages * stage, bn * 132 * 4) + 1024;
+            const int smem = splits > 1 ? kAllSmem : std::max(p.stages * stage, bn * 132 * 4) + 1024;
             s = launched(bn == 16 ? launch_tiles<16>(p, splits, smem, st) : bn == 32 ? launch_tiles<32>(p, splits, smem, st)
                          : bn == 64 ? launch_tiles<64>(p, splits, smem, st) : launch_tiles<128>(p, splits, smem, st));
         } else if (tiles[i] > sms / 2) {
-            static std::atomic<unsigned long long> done;
             if (!lay_out(prod + i, 1, 256, 256, 128, dtype, &p)) return err(FP_ERR_CUDA, refused);
-            const cudaError_t e = allow_smem(linear_pair_kernel, kPairSmem, &done);
-            s = launched(e != cudaSuccess ? e : launch_clusters(linear_pair_kernel, p, 2 * (sms / 2), kPairThreads, kPairSmem, 2, st));
+            s = launched(pairs(wide(i)));
         } else {
             // The tile's width and the pairs that share it by the cycles that they are expected to take: the K blocks, the exchange of
             // sums, finishing, and 3000 for everything else; a launch of more CTAs than run at once takes as many rounds.  Of
@@ -1035,7 +1134,9 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, int* sta
                     const int64_t ctas = 2 * c * ((prod[i].I + 255) / 256) * ((prod[i].J + b - 1) / b), room = std::min<int64_t>(share, split_room(c));
                     const double cost = (double)((ctas + room - 1) / room) *
                                         (3000 + (double)((kblocks + c - 1) / c) * (b == 256 ? 522 : 392) + 32.0 * b * (c - 1) / c + 11.0 * b / c);
-                    if (best == 0 || cost < best) { best = cost; bn = b; S = c; }
+                    // (a 32-bit result whose runs would be longer than twice kRun: only where there is no other way)
+                    const double much = p.run && (kblocks + c - 1) / c > 2 * kRun * (512 / b) ? 1e6 * (b / 128) / c : 0;
+                    if (best == 0 || cost + much < best) { best = cost + much; bn = b; S = c; }
                 }
             if (!lay_out(prod + i, 1, 256, bn, bn / 2, dtype, &p)) return err(FP_ERR_CUDA, refused);
             s = launched(bn == 256 ? launch_split<256>(p, S, st) : launch_split<128>(p, S, st));
