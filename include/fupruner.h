@@ -357,8 +357,11 @@ typedef struct {
 
 /*
  * fp_linear_forward - a fully connected layer: y = act(x w' + bias) + res (or act(x w' + bias + res)).
- * Products are summed in 32 bits on the tensor cores; bias, activation and residual are applied to the 32-bit sum, which
- * is rounded once.  What is not finite goes through by IEEE rules and stays in its row (x) or column (w, bias).
+ * Products are summed in 32 bits on the tensor cores, which cut sums toward zero; where y has 32 bits, in runs of 512 terms (as far as
+ * there is room for them) that are added with rounding: off by about 5e-7 then, by 1e-6 for every 1024 terms of a run otherwise.  Bias,
+ * activation and residual are applied to the 32-bit sum, which is rounded once.  gelu's Phi is off by 1.5e-7 at most.  What is not finite
+ * goes through by IEEE rules and stays in its row (x) or column (w, bias).  The order of sums depends on M, N, K, the types and the
+ * GPU alone: the same call gives the same bits.
  *   d_work, work_bytes   device scratch of at least fp_linear_workspace bytes, 256-byte aligned (NULL where that is 0).
  *               Two calls that may run at the same time need two; so do two captured graphs that may.
  * Errors: FP_ERR_ARG, FP_ERR_UNSUPPORTED (dtype), FP_ERR_BOUNDS (a size beyond 2^30, scratch too small), FP_ERR_CUDA.
@@ -386,21 +389,20 @@ typedef struct {
 /*
  * fp_linear_backward - the gradients of fp_linear_forward:
  *   dz = dy * act'(pre)      dx = dz w      dw = dz' x      db = sum of dz's rows
- * dz is computed in 32 bits; db sums it unrounded, the two products take it rounded to dtype.  Sums are taken in 32 bits
- * in an order that depends on the sizes alone: the same call gives the same bits.
+ * dz is computed in 32 bits; db sums it unrounded, the two products take it rounded to dtype.  Sums as in fp_linear_forward.
  * The derivative of relu at 0 is 0.  Scratch, streams and errors as in fp_linear_forward, with
  * fp_linear_backward_workspace.  At least one output must be given.
  */
 fp_status fp_linear_backward(const fp_linear_grad_args* args, void* d_work, size_t work_bytes, void* stream);
 
-/* Bytes of scratch that a call with these arguments needs (0 where every operand can be read in place: base address and
- * row stride multiples of 16 bytes, and for fp_linear_backward no activation and no single dz).  Host only; depends on
- * the sizes, the pointers' alignment and which pointers are NULL. */
+/* Bytes of scratch that a call with these arguments needs.  An operand of a product is read in place where its base address and its row
+ * stride are multiples of 16 bytes, and copied into scratch otherwise; dz is read from d_dz or, without an activation, from d_dy where those can be, and
+ * written into scratch otherwise.  Host only; depends on the sizes, the pointers' alignment, the strides and which pointers are NULL. */
 fp_status fp_linear_workspace(const fp_linear_args* args, size_t* bytes);
 fp_status fp_linear_backward_workspace(const fp_linear_grad_args* args, size_t* bytes);
 
-/* What a bounded device-side wait of fp_linear_forward / fp_linear_backward on the current device has met since the last
- * call: FP_OK or FP_ERR_TIMEOUT (those results are invalid) in *h_status; synchronises with the device's work. */
+/* What the bounded device-side waits of fp_linear_forward / fp_linear_backward on the current device have met since the last
+ * call: FP_OK or FP_ERR_TIMEOUT (those results are invalid) in *h_status; waits for the device's work, so not for use in a capture. */
 fp_status fp_linear_status(int32_t* h_status);
 
 typedef struct {
@@ -420,7 +422,7 @@ typedef struct {
 
 /*
  * fp_cross_entropy - softmax cross-entropy of every row, loss = -sum target log softmax(logits), and its gradient, in
- * one pass.  Sums and exponentials in 32 bits.  Logits of -inf have probability 0 (with smoothing they make the loss
+ * one pass.  Sums and exponentials in 32 bits; exponentials below 2^-126 count as 0.  Logits of -inf have probability 0 (with smoothing they make the loss
  * infinite, as the formula does); a row that is -inf throughout, or holds NaN or +inf, gives NaN in that row alone; so does a
  * label outside [0, classes) other than ignore_index.  At least one of d_loss, d_dlogits.
  * Errors: FP_ERR_ARG, FP_ERR_UNSUPPORTED (dtype), FP_ERR_BOUNDS (rows or classes beyond 2^30), FP_ERR_CUDA.
@@ -462,6 +464,7 @@ typedef struct {
  * e4m3(x / scale), scale = largest |x| of the block / 448, rounded to nearest even; of v the square root is kept, which halves
  * its exponent range (taken to 2^-22 of itself; v below 2^-126 counts as 0), and a positive one never becomes 0 (it takes the smallest code),
  * so that no step is divided by eps alone because of rounding.  The step itself uses m and v before they are rounded.
+ * A gradient that is not finite makes its element's p, m and v not finite, and an infinite one the states of its block.
  *   h_tensors   host; read before the call returns.  No two tensors may overlap.
  * Errors: FP_ERR_ARG, FP_ERR_UNSUPPORTED (dtype, state_bits), FP_ERR_BOUNDS (n beyond 2^40), FP_ERR_CUDA; they are found
  * before anything is launched, except FP_ERR_CUDA.

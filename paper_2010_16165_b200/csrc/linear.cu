@@ -99,59 +99,93 @@ __device__ __forceinline__ Epilogue held(const Epilogue& from) {
     asm volatile("" : "+r"(e.y_type), "+r"(e.pre_type), "+r"(e.res_type), "+r"(e.bias_type), "+r"(e.act), "+r"(e.res_first), "+r"(e.vec));
     return e;
 }
-// A lane's four outputs of a row: neighbours n .. n + 3 where four neighbours lie aligned in every buffer (VEC), or else n, n + 32, n + 64 and
-// n + 96, so that neighbouring lanes have neighbouring columns.
-template <bool VEC> __device__ __forceinline__ int column(int n, int i) { return VEC ? n + i : n + 32 * i; }
-
-template <bool VEC>
-__device__ __forceinline__ void bias4(const Epilogue& e, int n, int N, float (&b)[4]) {
+// A lane's C outputs of a row: neighbours n .. n + 3 where four neighbours lie aligned in every buffer (STRIDE 1), or else n, n + 32, ..., so that
+// neighbouring lanes have neighbouring columns.  What exists of them and of U rows is asked once, types once for all of them:
+// asked at every element, code that runs twice a launch was fetched for longer than it ran (829 x 2816 x 256 with an unaligned residual 44 us).
+template <int C, int STRIDE>
+__device__ __forceinline__ uint32_t columns_in(int n, int N) {
+    uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = e.bias && column<VEC>(n, i) < N ? load1(e.bias, column<VEC>(n, i), e.bias_type) : 0.0f;
+    for (int i = 0; i < C; ++i) m |= n + STRIDE * i < N ? 1u << i : 0u;
+    return m;
 }
-// The residual of U rows `step` apart, those below `end`.
-template <int U, bool VEC>
-__device__ __forceinline__ void fetch(const Epilogue& e, long long row, int step, long long end, int n, int N, float (&r)[U][4]) {
+template <int C, int STRIDE>
+__device__ __forceinline__ void bias_of(const Epilogue& e, int n, int N, float (&b)[C]) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) b[i] = e.bias && n + STRIDE * i < N ? load1(e.bias, n + STRIDE * i, e.bias_type) : 0.0f;
+}
+// The residual of U rows `step` apart, `rows` of which exist.
+template <int U, int C, int STRIDE>
+__device__ __forceinline__ void fetch(const Epilogue& e, long long row, int step, int rows, int n, uint32_t in, float (&r)[U][C]) {
     if (!e.res) return;
+    const int bytes = e.res_type == FP_DTYPE_F32 ? 4 : 2;
+    const char* from = static_cast<const char*>(e.res) + (row * e.ld_res + n) * bytes;
+    const long long hop = step * e.ld_res * bytes;
+    if (STRIDE == 1 && C == 4 && in == 15u) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (row + u * step < end) {
-            const long long at = (row + u * step) * e.ld_res;
-            if (VEC && n + 4 <= N) load4(e.res, at + n, e.res_type, r[u]);
-            else
+        for (int u = 0; u < U; ++u, from += hop)
+            if (u < rows) load4(from, 0, e.res_type, reinterpret_cast<float(&)[4]>(r[u]));
+    } else if (bytes == 4) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) if (column<VEC>(n, i) < N) r[u][i] = load1(e.res, at + column<VEC>(n, i), e.res_type);
-        }
+        for (int u = 0; u < U; ++u, from += hop)
+#pragma unroll
+            for (int i = 0; i < C; ++i) if (u < rows && (in >> i & 1u)) r[u][i] = reinterpret_cast<const float*>(from)[STRIDE * i];
+    } else {
+        uint16_t w[U][C];
+#pragma unroll
+        for (int u = 0; u < U; ++u, from += hop)
+#pragma unroll
+            for (int i = 0; i < C; ++i) w[u][i] = u < rows && (in >> i & 1u) ? reinterpret_cast<const uint16_t*>(from)[STRIDE * i] : (uint16_t)0;
+        const bool bf16 = e.res_type == FP_DTYPE_BF16;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < C; ++i) r[u][i] = bf16 ? __uint_as_float((uint32_t)w[u][i] << 16) : __half2float(__ushort_as_half(w[u][i]));
+    }
 }
-template <int U, bool VEC>
-__device__ __forceinline__ void put(void* to, long long ld, int type, long long row, int step, long long end, int n, int N, const float (&v)[U][4]) {
+template <int U, int C, int STRIDE>
+__device__ __forceinline__ void put(void* base, long long ld, int type, long long row, int step, int rows, int n, uint32_t in, const float (&v)[U][C]) {
+    const int bytes = type == FP_DTYPE_F32 ? 4 : 2;
+    char* to = static_cast<char*>(base) + (row * ld + n) * bytes;
+    const long long hop = step * ld * bytes;
+    if (STRIDE == 1 && C == 4 && in == 15u) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (row + u * step < end) {
-            const long long at = (row + u * step) * ld;
-            if (VEC && n + 4 <= N) store4(to, at + n, type, v[u]);
-            else
+        for (int u = 0; u < U; ++u, to += hop)
+            if (u < rows) store4(to, 0, type, reinterpret_cast<const float(&)[4]>(v[u]));
+    } else if (bytes == 4) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) if (column<VEC>(n, i) < N) store1(to, at + column<VEC>(n, i), type, v[u][i]);
-        }
+        for (int u = 0; u < U; ++u, to += hop)
+#pragma unroll
+            for (int i = 0; i < C; ++i) if (u < rows && (in >> i & 1u)) reinterpret_cast<float*>(to)[STRIDE * i] = v[u][i];
+    } else {
+        const bool bf16 = type == FP_DTYPE_BF16;
+#pragma unroll
+        for (int u = 0; u < U; ++u, to += hop)
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                const uint16_t h = bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v[u][i])) : __half_as_ushort(__float2half_rn(v[u][i]));
+                if (u < rows && (in >> i & 1u)) reinterpret_cast<uint16_t*>(to)[STRIDE * i] = h;
+            }
+    }
 }
 // The outputs from their sums v, biases b and residuals r.  `e` is the caller's own copy: its fields stay in registers.
-template <int U, bool VEC>
-__device__ __forceinline__ void finish(const Epilogue& e, long long row, int step, long long end, int n, int N, float (&v)[U][4], const float (&b)[4], const float (&r)[U][4]) {
+template <int U, int C, int STRIDE>
+__device__ __forceinline__ void finish(const Epilogue& e, long long row, int step, int rows, int n, uint32_t in, float (&v)[U][C], const float (&b)[C], const float (&r)[U][C]) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < C; ++i) {
             v[u][i] += b[i];
             if (e.res && e.res_first) v[u][i] += r[u][i];
         }
-    if (e.pre) put<U, VEC>(e.pre, e.ld_pre, e.pre_type, row, step, end, n, N, v);
+    if (e.pre) put<U, C, STRIDE>(e.pre, e.ld_pre, e.pre_type, row, step, rows, n, in, v);
     act_all(v, e.act);
     if (e.res && !e.res_first)
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[u][i] += r[u][i];
-    put<U, VEC>(e.y, e.ld_y, e.y_type, row, step, end, n, N, v);
+            for (int i = 0; i < C; ++i) v[u][i] += r[u][i];
+    put<U, C, STRIDE>(e.y, e.ld_y, e.y_type, row, step, rows, n, in, v);
 }
 // Four words of a row of sums: neighbours, or every 32nd.
 template <bool VEC>
@@ -176,9 +210,11 @@ template <int S, int U, bool VEC>
 __device__ __forceinline__ void finish_rows(const Epilogue& e, uint32_t base, int pitch, int r0, int step, int rows, long long row0, int n0, int N, uint32_t first,
                                             uint32_t every) {
     const int lane = threadIdx.x & 31, n = n0 + (VEC ? 4 * lane : lane);
+    constexpr int STRIDE = VEC ? 1 : 32;
     if (n >= N) return;
+    const uint32_t in = columns_in<4, STRIDE>(n, N);
     float bias[4];
-    bias4<VEC>(e, n, N, bias);
+    bias_of<4, STRIDE>(e, n, N, bias);
     auto sums = [&](int r, float (&v)[U][4]) {
         uint32_t at[U];
 #pragma unroll
@@ -223,9 +259,10 @@ __device__ __forceinline__ void finish_rows(const Epilogue& e, uint32_t base, in
 #pragma unroll 1
     for (int r = r0; r < rows; r += U * step) {
         float v[U][4], res[U][4];
-        fetch<U, VEC>(e, row0 + r, step, row0 + rows, n, N, res);
+        const int there = (rows - r + step - 1) / step;
+        fetch<U, 4, STRIDE>(e, row0 + r, step, there, n, in, res);
         sums(r, v);
-        finish<U, VEC>(e, row0 + r, step, row0 + rows, n, N, v, bias, res);
+        finish<U, 4, STRIDE>(e, row0 + r, step, there, n, in, v, bias, res);
     }
 }
 
@@ -403,33 +440,6 @@ struct PairCtrl {
     int abort_flag;
 };
 
-// Column n of the rows row .. row + 7 below `end`, from sums kEpiPitch words apart.
-__device__ __forceinline__ void finish_column(const Epilogue& e, long long row, long long end, int n, uint32_t from, float bias) {
-    float v[8], r[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-        if (e.res && row + u < end) r[u] = load1(e.res, (row + u) * e.ld_res + n, e.res_type);
-        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v[u]) : "r"(from + (uint32_t)(u * kEpiPitch) * 4u));
-    }
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-        v[u] += bias;
-        if (e.res && e.res_first) v[u] += r[u];
-    }
-    if (e.pre)
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (row + u < end) store1(e.pre, (row + u) * e.ld_pre + n, e.pre_type, v[u]);
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-        v[u] = act_of(v[u], e.act);
-        if (e.res && !e.res_first) v[u] += r[u];
-    }
-#pragma unroll
-    for (int u = 0; u < 8; ++u)
-        if (row + u < end) store1(e.y, (row + u) * e.ld_y + n, e.y_type, v[u]);
-}
-
 struct Place { const Problem* q; int i0, j0; };
 template <int BN>
 __device__ __forceinline__ Place pair_place(const TileParams& p, int tile_all) {
@@ -592,25 +602,35 @@ __global__ void __launch_bounds__(PairShape<RUNS>::kThreads, 1) linear_pair_kern
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(put + (uint32_t)i * 16u), "r"(v[4 * i]), "r"(v[4 * i + 1]), "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
                 __syncwarp();
                 if (e.vec) {                             // four rows at a time, eight lanes a row
-                    const int col = col0 + (lane & 7) * 4;
+                    const int col = col0 + (lane & 7) * 4, rows = w.q->I - row0 - (lane >> 3);
                     if (col < w.q->J) {
+                        const uint32_t in = columns_in<4, 1>(col, w.q->J);
                         float bias[4];
-                        bias4<true>(e, col, w.q->J, bias);
+                        bias_of<4, 1>(e, col, w.q->J, bias);
                         constexpr int U = RUNS ? 1 : 4;
 #pragma unroll 1
                         for (int r = 0; r < 8; r += U) {
                             float x[U][4], res[U][4];
-                            fetch<U, true>(e, row0 + (lane >> 3) + 4 * r, 4, w.q->I, col, w.q->J, res);
+                            const int there = (rows - 4 * r + 3) / 4;
+                            fetch<U, 4, 1>(e, row0 + (lane >> 3) + 4 * r, 4, there, col, in, res);
 #pragma unroll
                             for (int u = 0; u < U; ++u) lds4<true>(get + (uint32_t)(4 * (r + u)) * (kEpiPitch * 4), x[u]);
-                            finish<U, true>(e, row0 + (lane >> 3) + 4 * r, 4, w.q->I, col, w.q->J, x, bias, res);
+                            finish<U, 4, 1>(e, row0 + (lane >> 3) + 4 * r, 4, there, col, in, x, bias, res);
                         }
                     }
-                } else if (col0 + lane < w.q->J) {       // a lane a column, four rows in the places of four columns
+                } else if (col0 + lane < w.q->J) {       // a lane a column
                     const int col = col0 + lane;
-                    const float bias = e.bias ? load1(e.bias, col, e.bias_type) : 0.0f;
+                    float bias[1];
+                    bias_of<1, 1>(e, col, w.q->J, bias);
+                    constexpr int U = RUNS ? 8 : 16;
 #pragma unroll 1
-                    for (int r = 0; r < 32; r += 8) finish_column(e, row0 + r, w.q->I, col, buf + (uint32_t)(r * kEpiPitch + lane) * 4u, bias);
+                    for (int r = 0; r < 32; r += U) {
+                        float x[U][1], res[U][1];
+                        fetch<U, 1, 1>(e, row0 + r, 1, w.q->I - row0 - r, col, 1u, res);
+#pragma unroll
+                        for (int u = 0; u < U; ++u) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x[u][0]) : "r"(buf + (uint32_t)((r + u) * kEpiPitch + lane) * 4u));
+                        finish<U, 1, 1>(e, row0 + r, 1, w.q->I - row0 - r, col, 1u, x, bias, res);
+                    }
                 }
                 __syncwarp();
             }
@@ -813,7 +833,7 @@ __global__ void __launch_bounds__(256) copy_rows_kernel(const __grid_constant__ 
 
 // ---- dz and the bias's gradient -------------------------------------------------------------------------------------
 // dz = dy * act'(pre), rounded into up to two places, and its column sums.  A cluster of CTAs has 128 columns; each CTA takes a
-// range of rows, half a warp a row, eight columns a lane.  Column sums: a thread's rows, then the sixteen halves, then the CTAs, each
+// range of rows, half a warp a row, eight columns a lane.  Column sums: a thread's rows, then the halves of warps, then the CTAs, each
 // in order.  Memory bound: 6 bytes an element with an activation.
 
 struct DzParams {
@@ -825,9 +845,9 @@ struct DzParams {
     int N, act, dtype, db_type, accumulate, splits;
 };
 
-template <int DT, int ACT, bool VEC>
-__global__ void __launch_bounds__(256) linear_dz_kernel(const DzParams p) {
-    __shared__ float part[16][128];
+template <int DT, int ACT, bool VEC, int HALVES>
+__global__ void __launch_bounds__(16 * HALVES) linear_dz_kernel(const DzParams p) {
+    __shared__ float part[HALVES][128];
     __shared__ float sums[128];
     after_the_last(0);
     let_the_next_begin();
@@ -855,17 +875,17 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzParams p) {
     };
     constexpr int kRows = VEC ? 4 : 2;                   // rows a thread has in flight
 #pragma unroll 1
-    for (long long m = m0 + half; m < m1; m += 16 * kRows) {
+    for (long long m = m0 + half; m < m1; m += HALVES * kRows) {
         uint4 g[kRows], z[kRows];
 #pragma unroll
         for (int r = 0; r < kRows; ++r)
-            if (m + 16 * r < m1) {
-                g[r] = load(p.dy, (m + 16 * r) * p.ld_dy);
-                if (ACT != FP_ACT_NONE) z[r] = load(p.pre, (m + 16 * r) * p.ld_pre);
+            if (m + HALVES * r < m1) {
+                g[r] = load(p.dy, (m + HALVES * r) * p.ld_dy);
+                if (ACT != FP_ACT_NONE) z[r] = load(p.pre, (m + HALVES * r) * p.ld_pre);
             }
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
-            if (m + 16 * r >= m1) break;
+            if (m + HALVES * r >= m1) break;
             float d[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -877,7 +897,7 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzParams p) {
 #pragma unroll
             for (int o = 0; o < 2; ++o)
                 if (p.out[o]) {
-                    uint16_t* to = p.out[o] + (m + 16 * r) * p.ld_out[o];
+                    uint16_t* to = p.out[o] + (m + HALVES * r) * p.ld_out[o];
                     if (VEC) { if (col(0) < p.N) *reinterpret_cast<uint4*>(to + col(0)) = u; }
                     else
 #pragma unroll
@@ -892,7 +912,7 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzParams p) {
     float v = 0.0f;
     if (threadIdx.x < 128) {
 #pragma unroll
-        for (int w = 0; w < 16; ++w) v += part[w][threadIdx.x];
+        for (int w = 0; w < HALVES; ++w) v += part[w][threadIdx.x];
         sums[threadIdx.x] = v;
     }
     if (p.splits > 1) cluster_sync_all();
@@ -912,12 +932,15 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzParams p) {
 
 typedef void (*DzKernel)(const DzParams);
 template <int DT, int ACT>
-DzKernel dz_kernel(bool vec) { return vec ? linear_dz_kernel<DT, ACT, true> : linear_dz_kernel<DT, ACT, false>; }
+DzKernel dz_kernel(bool vec, bool narrow) {
+    return vec ? (narrow ? linear_dz_kernel<DT, ACT, true, 64> : linear_dz_kernel<DT, ACT, true, 16>)
+               : (narrow ? linear_dz_kernel<DT, ACT, false, 64> : linear_dz_kernel<DT, ACT, false, 16>);
+}
 template <int DT>
-DzKernel dz_kernel(int act, bool vec) {
-    return act == FP_ACT_RELU ? dz_kernel<DT, FP_ACT_RELU>(vec) : act == FP_ACT_GELU ? dz_kernel<DT, FP_ACT_GELU>(vec)
-         : act == FP_ACT_GELU_TANH ? dz_kernel<DT, FP_ACT_GELU_TANH>(vec) : act == FP_ACT_SILU ? dz_kernel<DT, FP_ACT_SILU>(vec)
-                                                                                         : dz_kernel<DT, FP_ACT_NONE>(vec);
+DzKernel dz_kernel(int act, bool vec, bool narrow) {
+    return act == FP_ACT_RELU ? dz_kernel<DT, FP_ACT_RELU>(vec, narrow) : act == FP_ACT_GELU ? dz_kernel<DT, FP_ACT_GELU>(vec, narrow)
+         : act == FP_ACT_GELU_TANH ? dz_kernel<DT, FP_ACT_GELU_TANH>(vec, narrow) : act == FP_ACT_SILU ? dz_kernel<DT, FP_ACT_SILU>(vec, narrow)
+                                                                                                 : dz_kernel<DT, FP_ACT_NONE>(vec, narrow);
 }
 
 // ---- host -----------------------------------------------------------------------------------------------------------
@@ -1345,8 +1368,10 @@ extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work
         while (d.splits < 8 && a->M > 32 * d.splits && blocks * d.splits < 8 * sm_count()) d.splits *= 2;
         const bool vec = (a->N & 7) == 0 && readable(a->d_dy, a->M, a->ld_dy) && (a->act == FP_ACT_NONE || readable(a->d_pre, a->M, a->ld_pre)) &&
                          (!a->d_dz || readable(a->d_dz, a->M, a->ld_dz));
-        const DzKernel k = a->dtype == FP_DTYPE_BF16 ? dz_kernel<FP_DTYPE_BF16>(a->act, vec) : dz_kernel<FP_DTYPE_F16>(a->act, vec);
-        if ((s = launched(launch_clusters(k, d, blocks * d.splits, 256, 0, d.splits, st))) != FP_OK) return s;
+        // few columns and many rows: the eight CTAs of a cluster are all there are, so they are large (4637 x 15 unaligned: 37 -> 19 us)
+        const bool narrow = blocks * d.splits * 4 <= sm_count() && a->M > 64 * d.splits;
+        const DzKernel k = a->dtype == FP_DTYPE_BF16 ? dz_kernel<FP_DTYPE_BF16>(a->act, vec, narrow) : dz_kernel<FP_DTYPE_F16>(a->act, vec, narrow);
+        if ((s = launched(launch_clusters(k, d, blocks * d.splits, narrow ? 1024 : 256, 0, d.splits, st))) != FP_OK) return s;
     }
     if (!a->d_dx && !a->d_dw) return FP_OK;
     CopyJob jobs[2];

@@ -132,16 +132,16 @@ __device__ __forceinline__ float act_grad(float z, int act) {
         default: return 1.0f;
     }
 }
-// Rows of four values, the choice made once for all of them.
-template <int ACT, int U>
-__device__ __forceinline__ void act_rows(float (&v)[U][4]) {
+// Rows of values, the choice made once for all of them.
+template <int ACT, int U, int C>
+__device__ __forceinline__ void act_rows(float (&v)[U][C]) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[u][i] = act_of(v[u][i], ACT);
+        for (int i = 0; i < C; ++i) v[u][i] = act_of(v[u][i], ACT);
 }
-template <int U>
-__device__ __forceinline__ void act_all(float (&v)[U][4], int act) {
+template <int U, int C>
+__device__ __forceinline__ void act_all(float (&v)[U][C], int act) {
     if (act == FP_ACT_RELU) act_rows<FP_ACT_RELU>(v);
     else if (act == FP_ACT_GELU) act_rows<FP_ACT_GELU>(v);
     else if (act == FP_ACT_GELU_TANH) act_rows<FP_ACT_GELU_TANH>(v);

@@ -347,6 +347,87 @@ def test_same_bits_every_time_and_under_capture(B):
         assert all(torch.equal(a, b) for a, b in zip(first, (y, dx, dw, db)))
 
 
+@pytest.mark.parametrize("M,N", [(4, 300), (100, 300), (300, 520), (2304, 2560)])
+def test_sums_in_32_bits_are_not_cut_short(B, M, N):
+    """The tensor cores cut a sum toward zero at every 16 terms, by 2^-23 of it at most.  A 32-bit result is summed in runs of 512 terms
+    (1024 where tensor memory holds no more runs): 64 cuts, so it is too small by 64 * 2^-23 of itself at most, not by 1024 * 2^-23 as 16384 terms in one run
+    could be (measured: 1.6e-5).  That is where every cut takes a whole unit of a sum of its final size; a cut takes half a unit on average,
+    of sums that grow up to that size: a quarter.  The runs' rounded sums have no direction."""
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    K = 16384
+    x, w = rows(gen, M, K, torch.bfloat16), rows(gen, N, K, torch.bfloat16, scale=K ** -0.5)
+    y = torch.empty(M, N, device="cuda")
+    B.fp_linear_forward(x, w, y)
+    z = x.double() @ w.double().t()
+    short = -((y.double() - z) * z.sign()).mean() / z.abs().mean()
+    assert short <= 64 * 2.0 ** -23 / 4 and (y.double() - z).norm() <= 64 * 2.0 ** -23 / 4 * z.norm()
+
+
+@pytest.mark.parametrize("M,N,K", [(3000, 10, 200), (5000, 16, 136), (2500, 100, 65), (9000, 3, 33), (700, 128, 64)])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+def test_gradients_of_narrow_layers(B, M, N, K, act):
+    backward_case(B, M, N, K, act=act, dz=True)
+    backward_case(B, M, N, K, dtype=F16, act=act, out=F16, want="xwb")
+
+
+def test_calls_that_follow_each_other_share_their_scratch(B):
+    """Twenty layers one after the other through one scratch buffer, each reading what the one before has written: launches that overlap
+    keep their order."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    for M, N in ((3, 65), (70, 129), (300, 131), (2000, 2051)):
+        w = [rows(gen, N, N, torch.bfloat16, pad=1, scale=N ** -0.5) for _ in range(4)]
+        x0 = rows(gen, M, N, torch.bfloat16, pad=1)
+        bufs = [torch.empty(M, N, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+        work = torch.empty(B.fp_linear_workspace(x0, w[0], bufs[0]) + B.fp_linear_workspace(bufs[0], w[0], bufs[1]), dtype=torch.uint8, device="cuda")
+
+        def run(wait):
+            x = x0
+            for i in range(20):
+                y = bufs[i % 2]
+                B.fp_linear_forward(x, w[i % 4], y, act=B.FP_ACT_SILU, res=x0, work=work)
+                if wait:
+                    torch.cuda.synchronize()
+                x = y
+            dx, dw = torch.empty(M, N, device="cuda", dtype=torch.bfloat16), torch.empty(N, N, device="cuda")
+            for i in range(6):
+                kw = dict(dx=dx, dw=dw, db=None, pre=x0, act=B.FP_ACT_SILU)
+                scratch = back if i % 2 else back2
+                B.fp_linear_backward(x, x0, w[i % 4], work=scratch, **kw)
+                B.fp_linear_forward(dx, w[0], x, work=work)
+                if wait:
+                    torch.cuda.synchronize()
+            return x.clone(), dx.clone(), dw.clone()
+        need = B.fp_linear_backward_workspace(bufs[1], x0, w[0], dx=bufs[0], dw=torch.empty(N, N, device="cuda"), pre=x0, act=B.FP_ACT_SILU)
+        back, back2 = (torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(2))
+        first = run(True)
+        for _ in range(3):
+            assert all(torch.equal(a, b) for a, b in zip(first, run(False)))
+
+
+def test_calls_of_every_form_on_two_streams(B):
+    """Single rows, small, split and large products queued on two streams at once give what they give alone."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    cases = []
+    for M, N, K in ((1, 1000, 2048), (40, 512, 4096), (300, 300, 4096), (1000, 777, 520), (2304, 2304, 512), (2, 8192, 512)):
+        x, w = rows(gen, M, K, torch.bfloat16), rows(gen, N, K, torch.bfloat16, scale=K ** -0.5)
+        y = torch.empty(M, N, device="cuda")
+        B.fp_linear_forward(x, w, y)
+        cases.append((x, w, y, y.clone()))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[torch.empty_like(c[2]) for c in cases] for _ in streams]
+    torch.cuda.synchronize()
+    for i in range(30):
+        for k, st in enumerate(streams):
+            j = (i * (k + 1) + k) % len(cases)
+            B.fp_linear_forward(cases[j][0], cases[j][1], outs[k][j], stream=st)
+    torch.cuda.synchronize()
+    for k in range(2):
+        for i in range(30):
+            j = (i * (k + 1) + k) % len(cases)
+            assert torch.equal(outs[k][j], cases[j][3])
+    assert B.fp_linear_status() == B.FP_OK
+
+
 def test_scratch_that_is_too_small_or_not_on_the_device_is_refused(B):
     x, w, y = (torch.zeros(s, device="cuda", dtype=torch.bfloat16) for s in ((200, 15), (8, 15), (200, 8)))
     need = B.fp_linear_workspace(x, w, y)
