@@ -305,6 +305,16 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
             mbar_init(done, 1);
             ctrl.abort_flag = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            // While the launch before ends, the first weights come into L2 (which is where memory is one: what that launch still
+            // writes of them is found there all the same).
+            for (int kb = kb0; kb < min(kb1, kb0 + p.stages); ++kb) {
+                if (q.a_mn) {
+                    tma_prefetch_2d(&q.a, i0, kb * kBlockK);
+                    tma_prefetch_2d(&q.a, i0 + 64, kb * kBlockK);
+                } else {
+                    tma_prefetch_2d(&q.a, kb * kBlockK, i0);
+                }
+            }
         }
     }
     after_the_last(p.late);

@@ -160,6 +160,10 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const void* map, 
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+// The same box into L2 only: a hint, which reads nothing that a later copy would not find as it is then.
+__device__ __forceinline__ void tma_prefetch_2d(const void* map, int x, int y) {
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(map), "r"(x), "r"(y) : "memory");
+}
 __device__ __forceinline__ void prefetch_map(const void* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
 // Operand descriptor words, 128-byte swizzle.  K-major: rows of 64 K elements, 8-row groups 1024 bytes apart; 16 K elements
