@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant
 // Half a warp has a block of 256 elements, sixteen a lane; the block's largest values come from shuffles.  With 16-bit parameters an
 // element is 10 bytes, for which the memory leaves 27 instructions, hence: two elements go through one packed instruction where there
 // is one (each half rounded as by itself), what a block needs once is paid for by sixteen elements, and the root is the approximate
-// one, off by 2^-22 of itself at most: with the exact one 315 M elements took 368 us instead of 318.
+// one, off by 2^-22 of itself at most: with the exact one 157 M elements took 368 us instead of 318.
 
 typedef unsigned long long Two;                          // two floats
 __device__ __forceinline__ Two two(float lo, float hi) { Two r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }

@@ -1004,8 +1004,8 @@ cudaError_t allow_smem(K kernel, int bytes, std::atomic<unsigned long long>* don
 struct Operand { const void* p; int64_t rows, cols, ld; int mn; };   // mn: rows are the sum's index
 struct Product { Operand a, b; int64_t I, J, Kc; int swap; Epilogue e; };
 
-// Fills in a launch's problems for tiles of ti x tj, B in boxes of box_b rows; false where a tensor map is refused, or there are more tiles than an index holds.
-bool lay_out(const Product* prod, int n, int ti, int tj, int box_b, int dtype, TileParams* p) {
+// Fills in a launch's problems for tiles of ti x tj, B in boxes of box_b rows.
+fp_status lay_out(const Product* prod, int n, int ti, int tj, int box_b, int dtype, TileParams* p) {
     int64_t tiles = 0;
     for (int i = 0; i < n; ++i) {
         const Product& r = prod[i];
@@ -1014,14 +1014,14 @@ bool lay_out(const Product* prod, int n, int ti, int tj, int box_b, int dtype, T
         q.tiles_i = (int)((r.I + ti - 1) / ti); q.tiles_j = (int)((r.J + tj - 1) / tj);
         q.tile0 = (int)tiles;
         tiles += (int64_t)q.tiles_i * q.tiles_j;
-        if (tiles > (1 << 27)) return false;
+        if (tiles > (1 << 27)) return err(FP_ERR_BOUNDS, "fp_linear: more tiles than a launch takes");
         q.a_mn = r.a.mn; q.b_mn = r.b.mn; q.e = r.e;
         if (!make_map(&q.a, r.a.p, r.a.rows, r.a.cols, r.a.ld, r.a.mn ? 64 : 128, dtype) ||
             !make_map(&q.b, r.b.p, r.b.rows, r.b.cols, r.b.ld, r.b.mn ? 64 : box_b, dtype))
-            return false;
+            return err(FP_ERR_CUDA, "fp_linear: an operand's tensor map was refused");
     }
     p->n_prob = n; p->tiles = (int)tiles;
-    return true;
+    return FP_OK;
 }
 
 // A launch in clusters that may begin while the launch before it ends (see after_the_last).
@@ -1107,8 +1107,8 @@ fp_status launched(cudaError_t e) {
 
 // The products of a call (two, or one); `late`: their operands were there before the launch in front of them began.
 fp_status run_products(const Product* prod, int n, int dtype, int late, int* status, cudaStream_t st) {
-    const char* refused = "fp_linear: an operand's tensor map was refused, or there are too many tiles";
     const int sms = sm_count();
+    fp_status s;
     TileParams p;
     memset(&p, 0, sizeof(p));
     p.status = status; p.bf16 = dtype == FP_DTYPE_BF16;
@@ -1129,30 +1129,29 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, int* sta
                     : launch_clusters(linear_pair_kernel<false>, p, 2 * (sms / 2), PairShape<false>::kThreads, kAllSmem, 2, st);
     };
     if (!few && tiles[0] + tiles[1] > sms / 2) {
-        if (!lay_out(prod, n, 256, 256, 128, dtype, &p)) return err(FP_ERR_CUDA, refused);
+        if ((s = lay_out(prod, n, 256, 256, 128, dtype, &p)) != FP_OK) return s;
         p.late = late;
         return launched(pairs(wide(0) || (n > 1 && wide(1))));
     }
     // one after the other, the second beside the first
     for (int i = 0; i < n; ++i) {
-        fp_status s;
         p.late = late || i > 0;
         p.run = wide(i) ? kRun : 0;
         if (prod[i].swap) {
             const int bn = prod[i].J <= 16 ? 16 : prod[i].J <= 32 ? 32 : prod[i].J <= 64 ? 64 : 128;
-            if (!lay_out(prod + i, 1, 128, bn, bn, dtype, &p)) return err(FP_ERR_CUDA, refused);
+            if ((s = lay_out(prod + i, 1, 128, bn, bn, dtype, &p)) != FP_OK) return s;
             const int kblocks = p.prob[0].kblocks;
             int splits = 1;
             const int most = p.run ? std::min(512 / bn, 16) : 1;       // accumulators
             while (splits < 8 && kblocks >= splits * 4 && (p.tiles * splits * 2 <= sms || (p.run && kblocks > 2 * kRun * most * splits))) splits *= 2;
             // (two CTAs on an SM share its 512 columns)
-            const int stage = 128 * 128 + bn * 128, room = p.tiles * splits > sms && most * bn <= 256 ? kMaxSmem / 2 - 3072 : kMaxSmem - 3072;
+            const int stage = 128 * 128 + bn * 128, room = p.tiles * splits > sms && most * bn <= 256 ? kAllSmem / 2 - 2048 : kAllSmem - 1024;
             p.stages = std::min(std::min(room / stage, 16), (kblocks + splits - 1) / splits);
             const int smem = splits > 1 ? kAllSmem : std::max(p.stages * stage, bn * 132 * 4) + 1024;
             s = launched(bn == 16 ? launch_tiles<16>(p, splits, smem, st) : bn == 32 ? launch_tiles<32>(p, splits, smem, st)
                          : bn == 64 ? launch_tiles<64>(p, splits, smem, st) : launch_tiles<128>(p, splits, smem, st));
         } else if (tiles[i] > sms / 2) {
-            if (!lay_out(prod + i, 1, 256, 256, 128, dtype, &p)) return err(FP_ERR_CUDA, refused);
+            if ((s = lay_out(prod + i, 1, 256, 256, 128, dtype, &p)) != FP_OK) return s;
             s = launched(pairs(wide(i)));
         } else {
             // The tile's width and the pairs that share it by the cycles that they are expected to take: the K blocks, the exchange of
@@ -1171,7 +1170,7 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, int* sta
                     const double much = p.run && (kblocks + c - 1) / c > 2 * kRun * (512 / b) ? 1e6 * (b / 128) / c : 0;
                     if (best == 0 || cost + much < best) { best = cost + much; bn = b; S = c; }
                 }
-            if (!lay_out(prod + i, 1, 256, bn, bn / 2, dtype, &p)) return err(FP_ERR_CUDA, refused);
+            if ((s = lay_out(prod + i, 1, 256, bn, bn / 2, dtype, &p)) != FP_OK) return s;
             s = launched(bn == 256 ? launch_split<256>(p, S, st) : launch_split<128>(p, S, st));
         }
         if (s != FP_OK) return s;
@@ -1228,6 +1227,9 @@ fp_status check(const fp_linear_args* a) {
     const uintptr_t odd = (uintptr_t)a->d_x | (uintptr_t)a->d_w | (uintptr_t)a->d_res | (uintptr_t)a->d_pre;
     if ((odd & 1) || ((uintptr_t)a->d_y & (uintptr_t)(elem_bytes(a->y_dtype) - 1)) || ((uintptr_t)a->d_bias & (uintptr_t)(elem_bytes(a->bias_dtype) - 1)))
         return err(FP_ERR_ARG, "fp_linear_forward: a buffer is not aligned to its elements");
+    if (a->d_y == a->d_x || a->d_y == a->d_w || a->d_y == a->d_bias || (a->d_pre && (a->d_pre == a->d_x || a->d_pre == a->d_w || a->d_pre == a->d_y || a->d_pre == a->d_res)) ||
+        (a->d_res == a->d_y && (a->y_dtype != a->dtype || (a->M > 1 && a->ld_res != a->ld_y))))
+        return err(FP_ERR_ARG, "fp_linear_forward: an output is an input (only y may be res, with its type and row stride) or another output");
     return FP_OK;
 }
 
@@ -1257,6 +1259,15 @@ fp_status check(const fp_linear_grad_args* a) {
     if (a->d_dz == a->d_dy && a->M > 1 && a->ld_dz != a->ld_dy) return err(FP_ERR_ARG, "fp_linear_backward: dz in dy's place needs dy's row stride");
     const uintptr_t odd = (uintptr_t)a->d_dy | (uintptr_t)a->d_pre | (uintptr_t)a->d_x | (uintptr_t)a->d_w | (uintptr_t)a->d_dx | (uintptr_t)a->d_dz;
     if (odd & 1) return err(FP_ERR_ARG, "fp_linear_backward: a buffer is not aligned to its elements");
+    // (dz may be dy, and nothing else that is written anything else)
+    const void* outs_of[4] = {a->d_dx, a->d_dw, a->d_db, a->d_dz};
+    for (int i = 0; i < 4; ++i) {
+        const void* o = outs_of[i];
+        if (!o) continue;
+        bool again = (o == a->d_dy && i != 3) || (a->act != FP_ACT_NONE && o == a->d_pre) || (a->d_dw && o == a->d_x) || (a->d_dx && o == a->d_w);
+        for (int j = 0; j < i; ++j) again = again || o == outs_of[j];
+        if (again) return err(FP_ERR_ARG, "fp_linear_backward: an output is an input (only dz may be dy) or another output");
+    }
     return FP_OK;
 }
 

@@ -67,7 +67,7 @@ DTYPES = [torch.float32, torch.bfloat16, torch.float16]
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("M,C", [(1, 1), (3, 2), (5, 10), (300, 100), (64, 1000), (33, 1001), (7, 4096), (9, 8191), (4, 32000), (150, 33333), (3, 131072),
-                                 (2, 150001), (1, 500003), (1000, 31), (20, 16384), (2000, 2500)])
+                                 (2, 150001), (1, 500003), (2, 880000), (1000, 31), (20, 16384), (2000, 2500)])
 def test_sizes(B, M, C, dtype):
     x, lab = logits(M, C, dtype)
     check(B, x, lab, scale=1.0 / M)

@@ -6,18 +6,19 @@ import pytest
 from paper_2010_16165_b200 import binding as B
 
 P = 1 << 20          # an address that is never read: every call below is refused, or only asked for its scratch
+X, W, Y, Z = (P * k for k in (2, 3, 4, 5))       # others
 
 
 def linear(**kw):
-    d = dict(M=4, N=8, K=16, dtype=B.FP_DTYPE_BF16, y_dtype=B.FP_DTYPE_BF16, bias_dtype=B.FP_DTYPE_F32, act=0, res_first=0, reserved=0, d_x=P, d_w=P,
-             d_bias=P, d_res=None, d_y=P, d_pre=None, ld_x=16, ld_w=16, ld_res=8, ld_y=8, ld_pre=8)
+    d = dict(M=4, N=8, K=16, dtype=B.FP_DTYPE_BF16, y_dtype=B.FP_DTYPE_BF16, bias_dtype=B.FP_DTYPE_F32, act=0, res_first=0, reserved=0, d_x=X, d_w=W,
+             d_bias=P, d_res=None, d_y=Y, d_pre=None, ld_x=16, ld_w=16, ld_res=8, ld_y=8, ld_pre=8)
     d.update(kw)
     return B.fp_linear_args(**d)
 
 
 def grads(**kw):
-    d = dict(M=4, N=8, K=16, dtype=B.FP_DTYPE_BF16, dw_dtype=B.FP_DTYPE_F32, act=0, accumulate=0, d_dy=P, d_pre=None, d_x=P, d_w=P, d_dx=P, d_dw=P,
-             d_db=P, d_dz=None, ld_dy=8, ld_pre=8, ld_x=16, ld_w=16, ld_dx=16, ld_dw=16, ld_dz=8)
+    d = dict(M=4, N=8, K=16, dtype=B.FP_DTYPE_BF16, dw_dtype=B.FP_DTYPE_F32, act=0, accumulate=0, d_dy=Y, d_pre=None, d_x=X, d_w=W, d_dx=P, d_dw=6 * P,
+             d_db=7 * P, d_dz=None, ld_dy=8, ld_pre=8, ld_x=16, ld_w=16, ld_dx=16, ld_dw=16, ld_dz=8)
     d.update(kw)
     return B.fp_linear_grad_args(**d)
 
@@ -51,7 +52,9 @@ def message():
     (dict(y_dtype=B.FP_DTYPE_F16), B.FP_ERR_UNSUPPORTED), (dict(bias_dtype=B.FP_DTYPE_F16), B.FP_ERR_UNSUPPORTED), (dict(act=5), B.FP_ERR_ARG),
     (dict(act=-1), B.FP_ERR_ARG), (dict(res_first=2), B.FP_ERR_ARG), (dict(reserved=1), B.FP_ERR_ARG), (dict(d_x=None), B.FP_ERR_ARG),
     (dict(d_w=None), B.FP_ERR_ARG), (dict(d_y=None), B.FP_ERR_ARG), (dict(ld_x=15), B.FP_ERR_ARG), (dict(ld_w=0), B.FP_ERR_ARG), (dict(ld_y=7), B.FP_ERR_ARG),
-    (dict(d_res=P, ld_res=7), B.FP_ERR_ARG), (dict(d_pre=P, ld_pre=-8), B.FP_ERR_ARG), (dict(d_x=P + 1), B.FP_ERR_ARG),
+    (dict(d_res=Z, ld_res=7), B.FP_ERR_ARG), (dict(d_pre=Z, ld_pre=-8), B.FP_ERR_ARG), (dict(d_x=P + 1), B.FP_ERR_ARG),
+    (dict(d_y=X), B.FP_ERR_ARG), (dict(d_y=W), B.FP_ERR_ARG), (dict(d_y=P), B.FP_ERR_ARG), (dict(d_pre=Y), B.FP_ERR_ARG), (dict(d_pre=X), B.FP_ERR_ARG),
+    (dict(d_pre=Z, d_res=Z), B.FP_ERR_ARG), (dict(d_res=Y, y_dtype=B.FP_DTYPE_F32), B.FP_ERR_ARG), (dict(d_res=Y, ld_res=9), B.FP_ERR_ARG),
     (dict(y_dtype=B.FP_DTYPE_F32, d_y=P + 2), B.FP_ERR_ARG), (dict(d_bias=P + 2), B.FP_ERR_ARG), (dict(ld_x=1 << 39), B.FP_ERR_ARG)])
 def test_linear(kw, status):
     a, n = linear(**kw), ctypes.c_size_t(77)
@@ -66,8 +69,10 @@ def test_linear(kw, status):
     (dict(dtype=B.FP_DTYPE_F32), B.FP_ERR_UNSUPPORTED), (dict(dw_dtype=B.FP_DTYPE_F16), B.FP_ERR_UNSUPPORTED), (dict(act=9), B.FP_ERR_ARG),
     (dict(accumulate=-1), B.FP_ERR_ARG), (dict(act=B.FP_ACT_GELU), B.FP_ERR_ARG), (dict(d_dy=None), B.FP_ERR_ARG), (dict(d_x=None), B.FP_ERR_ARG),
     (dict(d_w=None), B.FP_ERR_ARG), (dict(d_dx=None, d_dw=None, d_db=None), B.FP_ERR_ARG), (dict(ld_dy=7), B.FP_ERR_ARG), (dict(ld_x=8), B.FP_ERR_ARG),
-    (dict(ld_w=8), B.FP_ERR_ARG), (dict(ld_dx=8), B.FP_ERR_ARG), (dict(ld_dw=8), B.FP_ERR_ARG), (dict(d_dz=P, ld_dz=9), B.FP_ERR_ARG),
-    (dict(d_dw=P + 2), B.FP_ERR_ARG), (dict(d_dy=P + 1), B.FP_ERR_ARG), (dict(M=0, d_db=P + 2), B.FP_ERR_ARG)])
+    (dict(ld_w=8), B.FP_ERR_ARG), (dict(ld_dx=8), B.FP_ERR_ARG), (dict(ld_dw=8), B.FP_ERR_ARG), (dict(d_dz=Y, ld_dz=9), B.FP_ERR_ARG),
+    (dict(d_dx=Y), B.FP_ERR_ARG), (dict(d_dx=X), B.FP_ERR_ARG), (dict(d_dx=W), B.FP_ERR_ARG), (dict(d_dw=W), B.FP_ERR_ARG), (dict(d_dz=X), B.FP_ERR_ARG),
+    (dict(d_dw=P), B.FP_ERR_ARG), (dict(d_db=6 * P), B.FP_ERR_ARG), (dict(act=1, d_pre=Z, d_dz=Z), B.FP_ERR_ARG),
+    (dict(d_dw=Z + 2), B.FP_ERR_ARG), (dict(d_dy=P + 1), B.FP_ERR_ARG), (dict(M=0, d_db=P + 2), B.FP_ERR_ARG)])
 def test_linear_gradients(kw, status):
     a, n = grads(**kw), ctypes.c_size_t(77)
     assert B.lib().fp_linear_backward(ctypes.addressof(a), None, 0, None) == status
@@ -86,15 +91,15 @@ def test_scratch_of_linear():
         return -(-n // 256) * 256
     back = B.lib().fp_linear_backward_workspace
     assert need(linear()) == 0 and need(linear(M=0, d_x=None, d_y=None, d_w=None)) == 0
-    assert need(linear(d_x=P + 2)) == up(4 * 16 * 2)
+    assert need(linear(d_x=X + 2)) == up(4 * 16 * 2)
     assert need(linear(M=100, ld_x=17)) == up(100 * 16 * 2)
     assert need(linear(M=1, ld_x=17)) == 0
     assert need(linear(K=15, ld_x=15, ld_w=15, N=1000, ld_y=1000)) == up(4 * 16 * 2) + up(1000 * 16 * 2)
     assert need(grads(), back) == 0
-    assert need(grads(act=1, d_pre=P), back) == up(4 * 8 * 2)
-    assert need(grads(act=1, d_pre=P, d_dz=2 * P, ld_dz=8), back) == 0
-    assert need(grads(act=1, d_pre=P, d_dz=2 * P, ld_dz=9), back) == up(4 * 8 * 2)
-    assert need(grads(act=1, d_pre=P, d_dx=None, d_dw=None), back) == 0
+    assert need(grads(act=1, d_pre=Z), back) == up(4 * 8 * 2)
+    assert need(grads(act=1, d_pre=Z, d_dz=8 * P, ld_dz=8), back) == 0
+    assert need(grads(act=1, d_pre=Z, d_dz=8 * P, ld_dz=9), back) == up(4 * 8 * 2)
+    assert need(grads(act=1, d_pre=Z, d_dx=None, d_dw=None), back) == 0
     assert need(grads(ld_x=17, ld_w=17), back) == up(4 * 16 * 2) + up(8 * 16 * 2)
     assert need(grads(ld_x=17, ld_w=17, d_dw=None, d_db=None), back) == up(8 * 16 * 2)
     assert need(grads(M=0), back) == 0
