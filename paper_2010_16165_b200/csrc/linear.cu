@@ -1389,8 +1389,8 @@ extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work
         while (d.splits < 8 && a->M > 32 * d.splits && blocks * d.splits < 8 * sm_count()) d.splits *= 2;
         const bool vec = (a->N & 7) == 0 && readable(a->d_dy, a->M, a->ld_dy) && (a->act == FP_ACT_NONE || readable(a->d_pre, a->M, a->ld_pre)) &&
                          (!a->d_dz || readable(a->d_dz, a->M, a->ld_dz));
-        // few columns and many rows: the eight CTAs of a cluster are all there are, so they are large (4637 x 15 unaligned: 37 -> 19 us)
-        const bool narrow = blocks * d.splits * 4 <= sm_count() && a->M > 64 * d.splits;
+        // fewer CTAs than SMs, and many rows: they are large (4637 x 15 unaligned 37 -> 19 us, 32768 x 1024 with gelu 164 -> 52)
+        const bool narrow = blocks * d.splits <= sm_count() && a->M > 64 * d.splits;
         const DzKernel k = a->dtype == FP_DTYPE_BF16 ? dz_kernel<FP_DTYPE_BF16>(a->act, vec, narrow) : dz_kernel<FP_DTYPE_F16>(a->act, vec, narrow);
         if ((s = launched(launch_clusters(k, d, blocks * d.splits, narrow ? 1024 : 256, 0, d.splits, st))) != FP_OK) return s;
     }
