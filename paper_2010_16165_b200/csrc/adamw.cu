@@ -170,14 +170,7 @@ __global__ void __launch_bounds__(kThreads) adamw32_kernel(const __grid_constant
 // is one (each half rounded as by itself), what a block needs once is paid for by sixteen elements, and the root is the approximate
 // one, off by 2^-22 of itself at most: with the exact one 157 M elements took 368 us instead of 318.
 
-typedef unsigned long long Two;                          // two floats
-__device__ __forceinline__ Two two(float lo, float hi) { Two r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
-__device__ __forceinline__ Two twice(float x) { return two(x, x); }
-__device__ __forceinline__ void split(Two x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
-__device__ __forceinline__ Two mul2(Two a, Two b) { Two r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 // (A packed product and sum were contracted in spite of their .rn; as a 1 + b with a 1 that comes from the host they are not.)
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) { Two r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
-
 __device__ __forceinline__ Two e4m3_values(uint32_t codes) {       // of the two low bytes
     uint32_t h;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));

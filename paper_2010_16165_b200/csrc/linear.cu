@@ -862,10 +862,10 @@ __global__ void __launch_bounds__(16 * HALVES) linear_dz_kernel(const DzParams p
     after_the_last(0);
     let_the_next_begin();
     const int lane = threadIdx.x & 15, half = threadIdx.x >> 4;
-    const int split = (int)(blockIdx.x % (unsigned)p.splits);
+    const int share = (int)(blockIdx.x % (unsigned)p.splits);
     const int n0 = (int)(blockIdx.x / (unsigned)p.splits) * 128;
-    const long long m0 = p.M * split / p.splits, m1 = p.M * (split + 1) / p.splits;
-    float s[8] = {};
+    const long long m0 = p.M * share / p.splits, m1 = p.M * (share + 1) / p.splits;
+    Two s[4] = {};                                       // (zeros)
     // columns of a thread: eight neighbours, or (rows that are not aligned) every sixteenth
     auto col = [&](int i) { return n0 + (VEC ? 8 * lane + i : lane + 16 * i); };
     auto load = [&](const uint16_t* base, long long row) {
@@ -898,10 +898,11 @@ __global__ void __launch_bounds__(16 * HALVES) linear_dz_kernel(const DzParams p
             if (m + HALVES * r >= m1) break;
             float d[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                d[i] = value(g[r], i);
-                if (ACT != FP_ACT_NONE) d[i] *= act_grad(value(z[r], i), ACT);
-                s[i] += d[i];
+            for (int i = 0; i < 8; i += 2) {
+                Two x = two(value(g[r], i), value(g[r], i + 1));
+                if (ACT != FP_ACT_NONE) x = mul2(x, act_grad2<ACT>(two(value(z[r], i), value(z[r], i + 1))));
+                s[i / 2] = add2(s[i / 2], x);
+                split(x, d[i], d[i + 1]);
             }
             const uint4 u = make_uint4(to_16x2(d[0], d[1], DT), to_16x2(d[2], d[3], DT), to_16x2(d[4], d[5], DT), to_16x2(d[6], d[7], DT));
 #pragma unroll
@@ -917,7 +918,7 @@ __global__ void __launch_bounds__(16 * HALVES) linear_dz_kernel(const DzParams p
     }
     if (!p.db) return;                                   // (the same for all CTAs of a cluster)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) part[half][col(i) - n0] = s[i];
+    for (int i = 0; i < 8; i += 2) split(s[i / 2], part[half][col(i) - n0], part[half][col(i + 1) - n0]);
     __syncthreads();
     float v = 0.0f;
     if (threadIdx.x < 128) {
@@ -926,7 +927,7 @@ __global__ void __launch_bounds__(16 * HALVES) linear_dz_kernel(const DzParams p
         sums[threadIdx.x] = v;
     }
     if (p.splits > 1) cluster_sync_all();
-    if (split == 0 && threadIdx.x < 128) {
+    if (share == 0 && threadIdx.x < 128) {
         float u[8];
 #pragma unroll
         for (int c = 1; c < 8; ++c)

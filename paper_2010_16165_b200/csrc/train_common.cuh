@@ -82,63 +82,110 @@ __device__ __forceinline__ void store4(void* base, long long at, int dtype, cons
     else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + at) = make_uint2(to_16x2(v[0], v[1], dtype), to_16x2(v[2], v[3], dtype));
 }
 
-// ---- activations ----------------------------------------------------------------------------------------------------
-// tanh(u) = 1 - 2 / (1 + e^2u), so z/2 (1 + tanh u) = z / (1 + e^-2u): one exponential, and no cancellation where the result is
-// small.  e^-2u = inf gives z * 0, the limit.  Exponentials and reciprocals are the approximate ones (2 ulp): results are rounded to
-// 16 bits, and the epilogue of a product has some 30 instructions an element before it, not the tensor cores, sets the pace.
+// ---- two floats in a register pair ----------------------------------------------------------------------------------
 
+typedef unsigned long long Two;
+__device__ __forceinline__ Two two(float lo, float hi) { Two r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
+__device__ __forceinline__ Two twice(float x) { return two(x, x); }
+__device__ __forceinline__ void split(Two x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ Two mul2(Two a, Two b) { Two r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ Two add2(Two a, Two b) { Two r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) { Two r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+// 2^x and 1 / x of both (2 ulp; results below 2^-126 are 0)
+__device__ __forceinline__ Two exp2_of2(Two x) {
+    float a, b;
+    split(x, a, b);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(b));
+    return two(a, b);
+}
+__device__ __forceinline__ Two inverse2(Two x) {
+    float a, b;
+    split(x, a, b);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(a));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(b));
+    return two(a, b);
+}
+
+// ---- activations ----------------------------------------------------------------------------------------------------
+// Two values at a time, in packed instructions: the epilogue of a product and dz are instruction-bound where the activation takes 40 instructions a
+// value (dz of 8192 x 16384 with gelu 174 us, of which the memory needs 123).
+// tanh(u) = 1 - 2 / (1 + e^2u), so z/2 (1 + tanh u) = z / (1 + e^-2u): one exponential, and no cancellation where the result is
+// small.  e^-2u = inf gives z * 0, the limit.
+
+constexpr float kLog2E_ = 1.4426950408889634f;
 constexpr float kSqrt2OverPi2 = 1.5957691216057308f;       // 2 sqrt(2 / pi)
 constexpr float kInvSqrt2 = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 
-__device__ __forceinline__ float inverse(float x) {        // beyond 2^126: 0
-    float r;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
 // Phi(z), with e = e^(-z^2 / 2) left for the density: Abramowitz and Stegun, formula 7.1.26, erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2)
-// with t = 1 / (1 + p x) for x >= 0, off by 1.5e-7 at most; below zero nothing cancels.
-__device__ __forceinline__ float normal_cdf(float z, float& e) {
-    const float t = inverse(fmaf(0.3275911f * kInvSqrt2, fabsf(z), 1.0f));
-    e = __expf(-0.5f * z * z);
-    const float tail = 0.5f * e * t * fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
-    return z > 0.0f ? 1.0f - tail : tail;
+// with t = 1 / (1 + p x) for x >= 0, off by 1.5e-7 at most; half of it is the tail of Phi.
+__device__ __forceinline__ Two normal_cdf2(Two z, Two& e) {
+    float a, b;
+    split(z, a, b);
+    const Two t = inverse2(fma2(twice(0.3275911f * kInvSqrt2), two(fabsf(a), fabsf(b)), twice(1.0f)));
+    e = exp2_of2(mul2(mul2(z, z), twice(-0.5f * kLog2E_)));
+    Two q = fma2(twice(0.5f * 1.061405429f), t, twice(0.5f * -1.453152027f));
+    q = fma2(q, t, twice(0.5f * 1.421413741f));
+    q = fma2(q, t, twice(0.5f * -0.284496736f));
+    q = fma2(q, t, twice(0.5f * 0.254829592f));
+    float lo, hi;
+    split(mul2(mul2(q, t), e), lo, hi);
+    return two(a > 0.0f ? 1.0f - lo : lo, b > 0.0f ? 1.0f - hi : hi);
 }
-__device__ __forceinline__ float act_of(float z, int act) {
-    switch (act) {
-        case FP_ACT_RELU: return z < 0.0f ? 0.0f : z;       // NaN stays
-        case FP_ACT_GELU: { float e; return z * normal_cdf(z, e); }
-        case FP_ACT_GELU_TANH: return z * inverse(1.0f + __expf(-kSqrt2OverPi2 * (z + 0.044715f * z * z * z)));
-        case FP_ACT_SILU: return z * inverse(1.0f + __expf(-z));
-        default: return z;
+// 1 / (1 + e^-2u) of gelu_tanh, and z^2
+__device__ __forceinline__ Two tanh_gate2(Two z, Two& zz) {
+    zz = mul2(z, z);
+    return inverse2(add2(exp2_of2(mul2(mul2(fma2(zz, twice(0.044715f), twice(1.0f)), z), twice(-kSqrt2OverPi2 * kLog2E_))), twice(1.0f)));
+}
+__device__ __forceinline__ Two gate2(Two z) { return inverse2(add2(exp2_of2(mul2(z, twice(-kLog2E_))), twice(1.0f))); }      // 1 / (1 + e^-z)
+
+template <int ACT>
+__device__ __forceinline__ Two act2(Two z) {
+    if (ACT == FP_ACT_RELU) {
+        float a, b;
+        split(z, a, b);
+        return two(a < 0.0f ? 0.0f : a, b < 0.0f ? 0.0f : b);       // NaN stays
     }
+    Two x;
+    if (ACT == FP_ACT_GELU) return mul2(z, normal_cdf2(z, x));
+    if (ACT == FP_ACT_GELU_TANH) return mul2(z, tanh_gate2(z, x));
+    if (ACT == FP_ACT_SILU) return mul2(z, gate2(z));
+    return z;
 }
-__device__ __forceinline__ float act_grad(float z, int act) {
-    switch (act) {
-        case FP_ACT_RELU: return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
-        case FP_ACT_GELU: {
-            float e;
-            const float p = normal_cdf(z, e);
-            return fmaf(z * kInvSqrt2Pi, e, p);
-        }
-        case FP_ACT_GELU_TANH: {
-            // d/dz z s(2u) = s + z s (1 - s) 2u',  2u' = 2 sqrt(2/pi) (1 + 3 0.044715 z^2)
-            const float s = inverse(1.0f + __expf(-kSqrt2OverPi2 * (z + 0.044715f * z * z * z)));
-            return s + z * s * (1.0f - s) * kSqrt2OverPi2 * (1.0f + fminf(0.134145f * z * z, 1e30f));   // (0 times inf for a finite z)
-        }
-        case FP_ACT_SILU: {
-            const float s = inverse(1.0f + __expf(-z));
-            return s * (1.0f + z * (1.0f - s));
-        }
-        default: return 1.0f;
+template <int ACT>
+__device__ __forceinline__ Two act_grad2(Two z) {
+    if (ACT == FP_ACT_RELU) {
+        float a, b;
+        split(z, a, b);
+        return two(a > 0.0f ? 1.0f : (a <= 0.0f ? 0.0f : a), b > 0.0f ? 1.0f : (b <= 0.0f ? 0.0f : b));
     }
+    if (ACT == FP_ACT_GELU) {
+        Two e;
+        const Two p = normal_cdf2(z, e);
+        return fma2(mul2(z, twice(kInvSqrt2Pi)), e, p);
+    }
+    if (ACT == FP_ACT_GELU_TANH) {
+        // d/dz z s(2u) = s + z s (1 - s) 2u',  2u' = 2 sqrt(2/pi) (1 + 3 0.044715 z^2)
+        Two zz;
+        const Two s = tanh_gate2(z, zz);
+        float a, b;
+        split(mul2(zz, twice(0.134145f)), a, b);
+        const Two du = mul2(add2(two(fminf(a, 1e30f), fminf(b, 1e30f)), twice(1.0f)), twice(kSqrt2OverPi2));      // (0 times inf for a finite z)
+        return fma2(mul2(mul2(z, s), fma2(s, twice(-1.0f), twice(1.0f))), du, s);
+    }
+    if (ACT == FP_ACT_SILU) {
+        const Two s = gate2(z);
+        return mul2(s, fma2(z, fma2(s, twice(-1.0f), twice(1.0f)), twice(1.0f)));
+    }
+    return twice(1.0f);
 }
+
 // Rows of values, the choice made once for all of them.
 template <int ACT, int U, int C>
 __device__ __forceinline__ void act_rows(float (&v)[U][C]) {
+    static_assert(U * C % 2 == 0, "in pairs");
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < C; ++i) v[u][i] = act_of(v[u][i], ACT);
+    for (int i = 0; i < U * C; i += 2) split(act2<ACT>(two(v[i / C][i % C], v[(i + 1) / C][(i + 1) % C])), v[i / C][i % C], v[(i + 1) / C][(i + 1) % C]);
 }
 template <int U, int C>
 __device__ __forceinline__ void act_all(float (&v)[U][C], int act) {
@@ -147,5 +194,6 @@ __device__ __forceinline__ void act_all(float (&v)[U][C], int act) {
     else if (act == FP_ACT_GELU_TANH) act_rows<FP_ACT_GELU_TANH>(v);
     else if (act == FP_ACT_SILU) act_rows<FP_ACT_SILU>(v);
 }
+
 }  // namespace train
 }  // namespace fp
