@@ -329,7 +329,9 @@ fp_status fp_rank_filters_static(const float* d_filters, int32_t K, int32_t per_
  * buffer and the stream belong to the CURRENT device (FP_ERR_ARG for a buffer that is host memory or on another
  * device).  Matrices are row major; ld_* is the number of ELEMENTS from one row to the next, at least the row's length;
  * any alignment to the element's size is allowed.  Elements between a row's end and the next row are neither read
- * into a result nor written.  Outputs may not overlap inputs or each other unless a call says so.
+ * into a result nor written.  Outputs may not overlap inputs or each other unless a call says so (an output that IS
+ * another buffer of the call is refused with FP_ERR_ARG; other overlaps are not looked for).  Make the first call of each
+ * kind on a device outside a capture: it loads code.
  */
 
 enum { FP_ACT_NONE = 0, FP_ACT_RELU = 1,

@@ -856,7 +856,7 @@ struct DzParams {
 };
 
 template <int DT, int ACT, bool VEC, int HALVES>
-__global__ void __launch_bounds__(16 * HALVES) linear_dz_kernel(const DzParams p) {
+__global__ void __launch_bounds__(16 * HALVES, HALVES == 16 ? 4 : 1) linear_dz_kernel(const DzParams p) {
     __shared__ float part[HALVES][128];
     __shared__ float sums[128];
     after_the_last(0);

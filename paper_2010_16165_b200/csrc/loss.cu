@@ -55,6 +55,7 @@ struct Below {
         fix = far ? 1.0f : exp2_of(-fmaf(m, kLog2E, -c));
     }
     __device__ __forceinline__ float near_value(float x) const { return exp2_of(fmaf(x, kLog2E, -c)); }     // without fix
+    __device__ __forceinline__ Two near_values(Two x) const { return exp2_of2(fma2(x, twice(kLog2E), twice(-c))); }
     __device__ __forceinline__ float value(float x) const { return far ? exp_of(x - m) : near_value(x) * fix; }
 };
 
@@ -77,6 +78,7 @@ template <int DT> struct Unit {
         if (DT == FP_DTYPE_BF16) return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
         return __half2float(__ushort_as_half((uint16_t)(w[i >> 1] >> (16 * (i & 1)))));
     }
+    __device__ __forceinline__ static Two pair_at(const uint4& u, int i) { return two(get(u, i), get(u, i + 1)); }
     __device__ __forceinline__ static uint4 make(const float (&v)[8]) {
         if (DT == FP_DTYPE_F32) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
         return make_uint4(to_16x2(v[0], v[1], DT), to_16x2(v[2], v[3], DT), to_16x2(v[4], v[5], DT), to_16x2(v[6], v[7], DT));
@@ -131,12 +133,15 @@ __device__ __forceinline__ Part part_of(const uint4 (&u)[V], int used) {
             for (int k = 0; k < V; ++k)
                 if (k < used) a.s += e.value(U::get(u[k], i));
     } else {
+        Two s = twice(0.0f);
 #pragma unroll
         for (int k = 0; k < V; ++k)
             if (k < used)
 #pragma unroll
-                for (int i = 0; i < U::E; ++i) a.s += e.near_value(U::get(u[k], i));
-        a.s *= e.fix;
+                for (int i = 0; i < U::E; i += 2) s = add2(s, e.near_values(U::pair_at(u[k], i)));
+        float lo, hi;
+        split(s, lo, hi);
+        a.s = (lo + hi) * e.fix;
     }
     return a;
 }
@@ -205,6 +210,7 @@ struct Slope {
         off = r.g * (p.smoothing / (float)p.C);
     }
     __device__ __forceinline__ float near_value(float x) const { return fmaf(e.near_value(x), near_scale, -off); }
+    __device__ __forceinline__ Two near_values(Two x) const { return fma2(e.near_values(x), twice(near_scale), twice(-off)); }
     __device__ __forceinline__ float operator()(float x) const { return e.far ? fmaf(exp_of(x - e.m), scale, -off) : near_value(x); }
 };
 
@@ -272,7 +278,7 @@ __global__ void __launch_bounds__(256, 4) cross_entropy_kernel(const LossParams 
                     for (int i = 0; i < E; ++i) v[i] = slope(U::get(u[k], i));
             } else if (!r.ignored) {
 #pragma unroll
-                for (int i = 0; i < E; ++i) v[i] = slope.near_value(U::get(u[k], i));
+                for (int i = 0; i < E; i += 2) split(slope.near_values(U::pair_at(u[k], i)), v[i], v[i + 1]);
             }
             if (alike || G < 32) {
                 if (alike && n < units && full(n)) U::store(p.dx, to + (long long)n * E - shift, U::make(v));
@@ -354,14 +360,16 @@ __global__ void __launch_bounds__(512, 3) cross_entropy_kept_kernel(const LossPa
                 for (int i = 0; i < E; ++i) a.s += e.value(U::get(u, i));
             }
         } else {
-            float s[2] = {0.0f, 0.0f};
+            Two s = twice(0.0f);
 #pragma unroll 4
             for (int k = 0; k < count; ++k) {
                 const uint4 u = mine[k * G];
 #pragma unroll
-                for (int i = 0; i < E; ++i) s[i & 1] += e.near_value(U::get(u, i));
+                for (int i = 0; i < E; i += 2) s = add2(s, e.near_values(U::pair_at(u, i)));
             }
-            a.s = (s[0] + s[1]) * e.fix;
+            float lo, hi;
+            split(s, lo, hi);
+            a.s = (lo + hi) * e.fix;
         }
     }
     if (p.smoothing != 0.0f)
@@ -392,7 +400,7 @@ __global__ void __launch_bounds__(512, 3) cross_entropy_kept_kernel(const LossPa
                 const uint4 u = mine[k * G];
                 float v[8];
 #pragma unroll
-                for (int i = 0; i < E; ++i) v[i] = slope.near_value(U::get(u, i));
+                for (int i = 0; i < E; i += 2) split(slope.near_values(U::pair_at(u, i)), v[i], v[i + 1]);
                 __stcs(reinterpret_cast<uint4*>(dst), U::make(v));
                 dst += kStep * 16;
             }
