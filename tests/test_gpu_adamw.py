@@ -280,3 +280,33 @@ def test_host_buffers_are_refused(B):
         with pytest.raises(B.FpError) as e:
             B.fp_adamw_step(table, lr=1.0)
         assert e.value.status == B.FP_ERR_ARG
+
+
+def test_offsets_beyond_32_bits(B):
+    """One tensor of more than 2^31 elements: its last blocks are what the formula makes of them, alone and masked."""
+    n = (1 << 31) + 12345
+    for masked in (False, True):
+        gen = torch.Generator(device="cuda").manual_seed(13)
+        tail, _ = make(16 * BLOCK + 12345 % BLOCK, BF16, BF16, 8, gen)
+        k, blocks = tail["p"].numel(), -(-n // BLOCK)
+        at = n - k
+        assert at % BLOCK == 0
+        t = dict(p=torch.zeros(n, device="cuda", dtype=BF16), g=torch.zeros(n, device="cuda", dtype=BF16), m=torch.zeros(n, device="cuda", dtype=torch.uint8),
+                 v=torch.zeros(n, device="cuda", dtype=torch.uint8), m_scale=torch.zeros(blocks, device="cuda"), v_scale=torch.zeros(blocks, device="cuda"))
+        for key in ("p", "g", "m", "v"):
+            t[key][at:] = tail[key]
+        for key in ("m_scale", "v_scale"):
+            t[key][at // BLOCK:] = tail[key]
+        if masked:                                       # an entry an element; every third of the last is pruned
+            t["mask"] = torch.ones(n, device="cuda", dtype=torch.uint8)
+            t["mask"][at::3] = 0
+            tail["mask"] = t["mask"][at:].clone()
+        B.fp_adamw_step(B.fp_adamw_tensors([t]), **H)
+        B.fp_adamw_step(B.fp_adamw_tensors([tail]), **H)
+        torch.cuda.synchronize()
+        for key in ("p", "m", "v"):
+            assert torch.equal(t[key][at:], tail[key])
+        for key in ("m_scale", "v_scale"):
+            assert torch.equal(t[key][at // BLOCK:], tail[key])
+        assert not t["p"][:1 << 20].any() and not t["m_scale"][:1 << 12].any()
+        del t

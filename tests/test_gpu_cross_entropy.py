@@ -193,3 +193,19 @@ def test_no_rows_and_host_buffers(B):
         host = torch.zeros(64, dtype=torch.int64).pin_memory()
         setattr(a, field, host.data_ptr())
         assert B.lib().fp_cross_entropy(ctypes.addressof(a), None) == B.FP_ERR_ARG
+
+
+def test_offsets_beyond_32_bits(B):
+    M, C = 17000, 131072
+    x = torch.empty(M, C, device="cuda", dtype=torch.bfloat16).normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    lab = torch.arange(M, device="cuda") * 7 % C
+    loss = torch.empty(M, device="cuda")
+    last = x[-3:].clone()
+    B.fp_cross_entropy(x, lab, loss, dlogits=x)
+    X = last.double()
+    want = -torch.log_softmax(X, 1).gather(1, lab[-3:, None])[:, 0]
+    r = (C / 16 + 60) * 2.0 ** -22
+    assert ((loss[-3:].double() - want).abs() <= r + 2.0 ** -20 * (X.abs().amax(1) + want)).all()
+    p = torch.softmax(X, 1)
+    p[torch.arange(3, device="cuda"), lab[-3:]] -= 1
+    assert ((x[-3:].double() - p).abs() <= (2 * r + 2.0 ** -8) * p.abs() + 2.0 ** -126).all()

@@ -452,3 +452,31 @@ def test_host_buffers_are_refused(B):
         setattr(a, field, host.data_ptr())
         assert B.lib().fp_linear_forward(ctypes.addressof(a), None, 0, None) == B.FP_ERR_ARG
         assert b"current device" in B.lib().fp_last_error()
+
+
+def test_offsets_beyond_32_bits(B):
+    """A batch whose outputs, and a layer whose weights, pass 2^31 elements: the rows at both ends."""
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    for M, N, K in ((70000, 33000, 32), (9, 70000, 33000)):
+        x, w = rows(gen, M, K, torch.bfloat16), torch.randn(N, K, generator=gen, device="cuda", dtype=torch.bfloat16)
+        y = torch.empty(M, N, device="cuda", dtype=torch.bfloat16)
+        B.fp_linear_forward(x, w, y)
+        for part in (slice(0, 4), slice(M - 5, M)):
+            for cols in (slice(0, 300), slice(N - 300, N)):
+                z, S = x[part].double() @ w[cols].double().t(), x[part].double().abs() @ w[cols].double().abs().t()
+                assert ((y[part, cols].double() - z).abs() <= K * 2.0 ** -23 * S + half_step(torch.bfloat16, z)).all()
+        # and back: dz of that size, through scratch of that size
+        dx, dw = torch.empty(M, K, device="cuda", dtype=torch.bfloat16), torch.empty(N, K, device="cuda", dtype=torch.bfloat16)
+        kw = dict(dx=dx, dw=dw, pre=y, act=B.FP_ACT_RELU)
+        work = torch.empty(B.fp_linear_backward_workspace(y, x, w, **kw), dtype=torch.uint8, device="cuda")
+        B.fp_linear_backward(y, x, w, work=work, **kw)
+        d = y[M - 3:].double().clamp(min=0)
+        z, S = torch.zeros(3, K, dtype=torch.float64, device="cuda"), torch.zeros(3, K, dtype=torch.float64, device="cuda")
+        for a in range(0, N, 10000):
+            z += d[:, a:a + 10000] @ w[a:a + 10000].double()
+            S += d[:, a:a + 10000] @ w[a:a + 10000].double().abs()
+        assert ((dx[M - 3:].double() - z).abs() <= N * 2.0 ** -23 * S + half_step(torch.bfloat16, z)).all()
+        d = y[:, N - 3:].double().clamp(min=0)
+        z, S = d.t() @ x.double(), d.t() @ x.double().abs()
+        assert ((dw[N - 3:].double() - z).abs() <= M * 2.0 ** -23 * S + half_step(torch.bfloat16, z)).all()
+        del x, w, y, dx, dw, work
