@@ -16,7 +16,6 @@
 
 #include <algorithm>
 #include <atomic>
-#include <mutex>
 
 namespace fp {
 namespace {
@@ -52,6 +51,14 @@ struct Problem {
     int a_mn, b_mn;
     Epilogue e;
 };
+struct DzParams {
+    const uint16_t* dy;
+    const uint16_t* pre;
+    uint16_t* out[2];
+    void* db;
+    long long ld_dy, ld_pre, ld_out[2], M;
+    int N, act, dtype, db_type, accumulate, splits;
+};
 struct TileParams {
     Problem prob[2];
     int n_prob, stages, tiles;
@@ -59,6 +66,8 @@ struct TileParams {
     int late;                                            // this launch's operands were there before the launch in front of it began: see after_the_last()
     uint32_t bf16;
     int* status;
+    DzParams sums;                                       // linear_split_kernel: column sums of dy, by clusters behind the tiles'
+    int sums_vec;
 };
 
 // Bounded wait by polling.  (A try_wait with a time hint sleeps in steps of 2.05 us here: products of some microseconds took whole
@@ -662,6 +671,92 @@ __global__ void __launch_bounds__(PairShape<RUNS>::kThreads, 1) linear_pair_kern
     before_the_end(p.late);
 }
 
+// ---- dz and the bias's gradient -------------------------------------------------------------------------------------
+// dz = dy * act'(pre), rounded into up to two places, and its column sums.  A cluster of CTAs has 128 columns; each CTA takes a
+// range of rows, half a warp a row, eight columns a lane.  Column sums: a thread's rows, then the halves of warps, then the CTAs, each
+// in order.  Memory bound: 6 bytes an element with an activation.
+// Where there is nothing but column sums to take, a product's launch takes them along (linear_split_kernel).
+
+template <int DT, int ACT, bool VEC, int HALVES>
+__device__ __forceinline__ void dz_columns(const DzParams& p, int block, int share, float (*part)[128], float* sums) {
+    const int lane = threadIdx.x & 15, half = threadIdx.x >> 4, n0 = block * 128;
+    const long long m0 = p.M * share / p.splits, m1 = p.M * (share + 1) / p.splits;
+    Two s[4] = {};                                       // (zeros)
+    // columns of a thread: eight neighbours, or (rows that are not aligned) every sixteenth
+    auto col = [&](int i) { return n0 + (VEC ? 8 * lane + i : lane + 16 * i); };
+    auto load = [&](const uint16_t* base, long long row) {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (VEC) { if (col(0) < p.N) u = __ldcs(reinterpret_cast<const uint4*>(base + row + col(0))); }
+        else {
+            uint32_t w[4] = {};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (col(i) < p.N) w[i >> 1] |= (uint32_t)base[row + col(i)] << (16 * (i & 1));
+            u = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        return u;
+    };
+    auto value = [](const uint4& u, int i) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        return to_f32((uint16_t)(w[i >> 1] >> (16 * (i & 1))), DT);
+    };
+    constexpr int kRows = VEC ? 4 : 2;                   // rows a thread has in flight
+#pragma unroll 1
+    for (long long m = m0 + half; m < m1; m += HALVES * kRows) {
+        uint4 g[kRows], z[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            if (m + HALVES * r < m1) {
+                g[r] = load(p.dy, (m + HALVES * r) * p.ld_dy);
+                if (ACT != FP_ACT_NONE) z[r] = load(p.pre, (m + HALVES * r) * p.ld_pre);
+            }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (m + HALVES * r >= m1) break;
+            float d[8];
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                Two x = two(value(g[r], i), value(g[r], i + 1));
+                if (ACT != FP_ACT_NONE) x = mul2(x, act_grad2<ACT>(two(value(z[r], i), value(z[r], i + 1))));
+                s[i / 2] = add2(s[i / 2], x);
+                split(x, d[i], d[i + 1]);
+            }
+            const uint4 u = make_uint4(to_16x2(d[0], d[1], DT), to_16x2(d[2], d[3], DT), to_16x2(d[4], d[5], DT), to_16x2(d[6], d[7], DT));
+#pragma unroll
+            for (int o = 0; o < 2; ++o)
+                if (p.out[o]) {
+                    uint16_t* to = p.out[o] + (m + HALVES * r) * p.ld_out[o];
+                    if (VEC) { if (col(0) < p.N) *reinterpret_cast<uint4*>(to + col(0)) = u; }
+                    else
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) if (col(i) < p.N) to[col(i)] = to_16(d[i], DT);
+                }
+        }
+    }
+    if (!p.db) return;                                   // (the same for all CTAs of a cluster)
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) split(s[i / 2], part[half][col(i) - n0], part[half][col(i + 1) - n0]);
+    __syncthreads();
+    float v = 0.0f;
+    if (threadIdx.x < 128) {
+#pragma unroll
+        for (int w = 0; w < HALVES; ++w) v += part[w][threadIdx.x];
+        sums[threadIdx.x] = v;
+    }
+    if (p.splits > 1) cluster_sync_all();
+    if (share == 0 && threadIdx.x < 128) {
+        float u[8];
+#pragma unroll
+        for (int c = 1; c < 8; ++c)
+            if (c < p.splits) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u[c]) : "r"(cluster_addr(smem_u32(&sums[threadIdx.x]), (uint32_t)c)));
+#pragma unroll
+        for (int c = 1; c < 8; ++c)
+            if (c < p.splits) v += u[c];
+        const int n = n0 + (int)threadIdx.x;
+        if (n < p.N) store1(p.db, n, p.db_type, p.accumulate ? load1(p.db, n, p.db_type) + v : v);
+    }
+    if (p.splits > 1) cluster_sync_all();
+}
+
 // ---- 256 x BN tiles with the sum split over pairs -----------------------------------------------------------------------
 // Products of fewer tiles than there are pairs: S pairs (a cluster of 2 S CTAs) share a tile's sum, as with few rows.
 // An SM takes 64 bytes a cycle from L2, so tiles are what counts: 32 KB a K block for 512 cycles of the tensor cores at BN = 256, 24 KB (392
@@ -691,7 +786,20 @@ __global__ void __launch_bounds__(kSplitThreads, 1) linear_split_kernel(const __
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_rank(), half = rank & 1u, first = rank & ~1u;      // this CTA's place in its pair, and the pair's first CTA
     const int split = (int)(rank >> 1);
-    const Place w = pair_place<BN>(p, (int)(blockIdx.x / (unsigned)(2 * S)));
+    const int cluster = (int)(blockIdx.x / (unsigned)(2 * S));
+    if (cluster >= p.tiles) {                            // columns of dy to be summed
+        float (*part)[128] = reinterpret_cast<float (*)[128]>(smem_raw);
+        float* sums = reinterpret_cast<float*>(smem_raw) + 32 * 128;
+        after_the_last(p.late);
+        let_the_next_begin();
+        if (p.bf16 && p.sums_vec) dz_columns<FP_DTYPE_BF16, FP_ACT_NONE, true, 32>(p.sums, cluster - p.tiles, (int)rank, part, sums);
+        else if (p.bf16) dz_columns<FP_DTYPE_BF16, FP_ACT_NONE, false, 32>(p.sums, cluster - p.tiles, (int)rank, part, sums);
+        else if (p.sums_vec) dz_columns<FP_DTYPE_F16, FP_ACT_NONE, true, 32>(p.sums, cluster - p.tiles, (int)rank, part, sums);
+        else dz_columns<FP_DTYPE_F16, FP_ACT_NONE, false, 32>(p.sums, cluster - p.tiles, (int)rank, part, sums);
+        before_the_end(p.late);
+        return;
+    }
+    const Place w = pair_place<BN>(p, cluster);
     const Problem& q = *w.q;
     const int i0 = w.i0 + 128 * (int)half;
     const int kb0 = (int)((long long)q.kblocks * split / S), kb1 = (int)((long long)q.kblocks * (split + 1) / S);
@@ -844,19 +952,7 @@ __global__ void __launch_bounds__(256) copy_rows_kernel(const __grid_constant__ 
         if (c0 + 32 * i < j.cols) d[c0 + 32 * i] = v[i];
 }
 
-// ---- dz and the bias's gradient -------------------------------------------------------------------------------------
-// dz = dy * act'(pre), rounded into up to two places, and its column sums.  A cluster of CTAs has 128 columns; each CTA takes a
-// range of rows, half a warp a row, eight columns a lane.  Column sums: a thread's rows, then the halves of warps, then the CTAs, each
-// in order.  Memory bound: 6 bytes an element with an activation.
-
-struct DzParams {
-    const uint16_t* dy;
-    const uint16_t* pre;
-    uint16_t* out[2];
-    void* db;
-    long long ld_dy, ld_pre, ld_out[2], M;
-    int N, act, dtype, db_type, accumulate, splits;
-};
+// ---- dz by itself ----------------------------------------------------------------------------------------------------
 
 template <int DT, int ACT, bool VEC, int HALVES>
 __global__ void __launch_bounds__(16 * HALVES, HALVES == 16 ? 4 : 1) linear_dz_kernel(const DzParams p) {
@@ -864,84 +960,7 @@ __global__ void __launch_bounds__(16 * HALVES, HALVES == 16 ? 4 : 1) linear_dz_k
     __shared__ float sums[128];
     after_the_last(0);
     let_the_next_begin();
-    const int lane = threadIdx.x & 15, half = threadIdx.x >> 4;
-    const int share = (int)(blockIdx.x % (unsigned)p.splits);
-    const int n0 = (int)(blockIdx.x / (unsigned)p.splits) * 128;
-    const long long m0 = p.M * share / p.splits, m1 = p.M * (share + 1) / p.splits;
-    Two s[4] = {};                                       // (zeros)
-    // columns of a thread: eight neighbours, or (rows that are not aligned) every sixteenth
-    auto col = [&](int i) { return n0 + (VEC ? 8 * lane + i : lane + 16 * i); };
-    auto load = [&](const uint16_t* base, long long row) {
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (VEC) { if (col(0) < p.N) u = __ldcs(reinterpret_cast<const uint4*>(base + row + col(0))); }
-        else {
-            uint32_t w[4] = {};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) if (col(i) < p.N) w[i >> 1] |= (uint32_t)base[row + col(i)] << (16 * (i & 1));
-            u = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        return u;
-    };
-    auto value = [](const uint4& u, int i) {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-        return to_f32((uint16_t)(w[i >> 1] >> (16 * (i & 1))), DT);
-    };
-    constexpr int kRows = VEC ? 4 : 2;                   // rows a thread has in flight
-#pragma unroll 1
-    for (long long m = m0 + half; m < m1; m += HALVES * kRows) {
-        uint4 g[kRows], z[kRows];
-#pragma unroll
-        for (int r = 0; r < kRows; ++r)
-            if (m + HALVES * r < m1) {
-                g[r] = load(p.dy, (m + HALVES * r) * p.ld_dy);
-                if (ACT != FP_ACT_NONE) z[r] = load(p.pre, (m + HALVES * r) * p.ld_pre);
-            }
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            if (m + HALVES * r >= m1) break;
-            float d[8];
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                Two x = two(value(g[r], i), value(g[r], i + 1));
-                if (ACT != FP_ACT_NONE) x = mul2(x, act_grad2<ACT>(two(value(z[r], i), value(z[r], i + 1))));
-                s[i / 2] = add2(s[i / 2], x);
-                split(x, d[i], d[i + 1]);
-            }
-            const uint4 u = make_uint4(to_16x2(d[0], d[1], DT), to_16x2(d[2], d[3], DT), to_16x2(d[4], d[5], DT), to_16x2(d[6], d[7], DT));
-#pragma unroll
-            for (int o = 0; o < 2; ++o)
-                if (p.out[o]) {
-                    uint16_t* to = p.out[o] + (m + HALVES * r) * p.ld_out[o];
-                    if (VEC) { if (col(0) < p.N) *reinterpret_cast<uint4*>(to + col(0)) = u; }
-                    else
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) if (col(i) < p.N) to[col(i)] = to_16(d[i], DT);
-                }
-        }
-    }
-    if (!p.db) return;                                   // (the same for all CTAs of a cluster)
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) split(s[i / 2], part[half][col(i) - n0], part[half][col(i + 1) - n0]);
-    __syncthreads();
-    float v = 0.0f;
-    if (threadIdx.x < 128) {
-#pragma unroll
-        for (int w = 0; w < HALVES; ++w) v += part[w][threadIdx.x];
-        sums[threadIdx.x] = v;
-    }
-    if (p.splits > 1) cluster_sync_all();
-    if (share == 0 && threadIdx.x < 128) {
-        float u[8];
-#pragma unroll
-        for (int c = 1; c < 8; ++c)
-            if (c < p.splits) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u[c]) : "r"(cluster_addr(smem_u32(&sums[threadIdx.x]), (uint32_t)c)));
-#pragma unroll
-        for (int c = 1; c < 8; ++c)
-            if (c < p.splits) v += u[c];
-        const int n = n0 + (int)threadIdx.x;
-        if (n < p.N) store1(p.db, n, p.db_type, p.accumulate ? load1(p.db, n, p.db_type) + v : v);
-    }
-    if (p.splits > 1) cluster_sync_all();
+    dz_columns<DT, ACT, VEC, HALVES>(p, (int)(blockIdx.x / (unsigned)p.splits), (int)(blockIdx.x % (unsigned)p.splits), part, sums);
 }
 
 typedef void (*DzKernel)(const DzParams);
@@ -1067,7 +1086,7 @@ template <int BN, int S>
 cudaError_t launch_split_of(const TileParams& p, cudaStream_t st) {
     static std::atomic<unsigned long long> done;
     const cudaError_t e = allow_smem(linear_split_kernel<BN, S>, kAllSmem, &done);
-    return e != cudaSuccess ? e : launch_clusters(linear_split_kernel<BN, S>, p, 2 * p.tiles * S, kSplitThreads, kAllSmem, 2 * S, st);
+    return e != cudaSuccess ? e : launch_clusters(linear_split_kernel<BN, S>, p, 2ll * (p.tiles + (p.sums.db ? (p.sums.N + 127) / 128 : 0)) * S, kSplitThreads, kAllSmem, 2 * S, st);
 }
 template <int BN>
 cudaError_t launch_split(const TileParams& p, int S, cudaStream_t st) {
@@ -1109,21 +1128,62 @@ fp_status launched(cudaError_t e) {
     return err(FP_ERR_CUDA, cudaGetErrorString(e));
 }
 
-// The products of a call (two, or one); `late`: their operands were there before the launch in front of them began.
-fp_status run_products(const Product* prod, int n, int dtype, int late, int* status, cudaStream_t st) {
+// See kRun.
+bool wide(const Product& r) { return r.e.y_type == FP_DTYPE_F32 && r.Kc > (int64_t)kRun * kBlockK; }
+int64_t blocks_of(const Product& r) { return (r.Kc + kBlockK - 1) / kBlockK; }
+int64_t tiles_of(const Product& r, int bn) { return ((r.I + 255) / 256) * ((r.J + bn - 1) / bn); }
+
+// How linear_split_kernel takes a product that has `share` of the SMs: the tile's width and the pairs that share it by the cycles that they are
+// expected to take: the K blocks, the exchange of sums, finishing, and 3000 for everything else; a launch of more CTAs than run at once takes
+// as many rounds.  `extra`: clusters of the launch that sum columns.
+struct SplitChoice { int bn, S; int64_t ctas; bool fits; };
+SplitChoice split_choice(const Product& r, int64_t share, int64_t extra) {
+    const int64_t kblocks = blocks_of(r);
+    SplitChoice best = {256, 1, 0, false};
+    double least = 0;
+    for (int b = 256; b >= 128; b /= 2)
+        for (int c = 1; c <= kMaxSplits && 2 * c <= std::max<int64_t>(kblocks, 2); ++c) {
+            const int64_t ctas = 2 * c * (tiles_of(r, b) + extra), room = std::min<int64_t>(share, split_room(c));
+            // (a 32-bit result whose runs would be longer than twice kRun: only where there is no other way)
+            const double much = wide(r) && (kblocks + c - 1) / c > 2 * kRun * (512 / b) ? 1e6 * (b / 128) / c : 0;
+            const double cost = much + (double)((ctas + room - 1) / room) *
+                                (3000 + (double)((kblocks + c - 1) / c) * (b == 256 ? 522 : 392) + 32.0 * b * (c - 1) / c + 11.0 * b / c);
+            if (least == 0 || cost < least) { least = cost; best = {b, c, ctas, ctas <= room}; }
+        }
+    return best;
+}
+
+// A call's products, one after the other, the second beside the first: the first has its share of the SMs by its work, the second what is
+// left, or its share.  (With few rows, where linear_tile_kernel takes the first, all of them.)
+int64_t share_of(const Product* prod, int n, int i, int64_t used) {
+    const int sms = sm_count();
+    if (n < 2 || prod[0].swap) return sms;
+    const int64_t w0 = tiles_of(prod[0], 256) * blocks_of(prod[0]), w1 = tiles_of(prod[1], 256) * blocks_of(prod[1]);
+    return std::max<int64_t>(i ? sms - used : 2, std::max<int64_t>(2, sms * (i ? w1 : w0) / (w0 + w1)));
+}
+
+// Whether a call's last product runs in linear_split_kernel with room for `extra` clusters that sum columns: beside the tiles, in one round
+// (300 x 2048 x 1000, where they do not fit: 17.8 us with them, 13.3 with a launch in front).  With few rows the first product's CTAs are
+// short, and need not leave room (64 x 512 x 512 8.8 -> 6.9 us, 64 x 2048 x 1024 14.0 -> 9.8, 64 x 1000 x 2048 14.0 -> 14.9).
+bool room_for_sums(const Product* prod, int n, int64_t extra) {
+    if (n == 0 || prod[n - 1].swap) return false;
+    const bool few = prod[0].swap;
+    if ((few || n < 2 ? tiles_of(prod[n - 1], 256) : tiles_of(prod[0], 256) + tiles_of(prod[1], 256)) + extra > sm_count() / 2) return false;
+    const int64_t used = n > 1 && !few ? split_choice(prod[0], share_of(prod, n, 0, 0), 0).ctas : 0;
+    return split_choice(prod[n - 1], share_of(prod, n, n - 1, used), extra).fits;
+}
+
+// The products of a call (two, or one); `late`: their operands were there before the launch in front of them began; `sums`: column sums that the
+// last one takes along, or nullptr.
+fp_status run_products(const Product* prod, int n, int dtype, int late, const DzParams* sums, int sums_vec, int* status, cudaStream_t st) {
     const int sms = sm_count();
     fp_status s;
     TileParams p;
     memset(&p, 0, sizeof(p));
     p.status = status; p.bf16 = dtype == FP_DTYPE_BF16;
-    bool few = prod[0].swap;
-    int64_t tiles[2] = {0, 0}, work = 0;
-    for (int i = 0; i < n; ++i) {
-        few = few || prod[i].swap;
-        tiles[i] = ((prod[i].I + 255) / 256) * ((prod[i].J + 255) / 256);
-        work += tiles[i] * ((prod[i].Kc + kBlockK - 1) / kBlockK);
-    }
-    auto wide = [&](int i) { return prod[i].e.y_type == FP_DTYPE_F32 && prod[i].Kc > (int64_t)kRun * kBlockK; };      // see kRun
+    const bool few = prod[0].swap;
+    int64_t tiles[2] = {0, 0}, used = 0;                 // tiles; CTAs of the first product
+    for (int i = 0; i < n; ++i) tiles[i] = tiles_of(prod[i], 256);
     auto pairs = [&](bool runs) -> cudaError_t {
         static std::atomic<unsigned long long> done[2];
         p.run = runs ? kRun : 0;
@@ -1135,12 +1195,12 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, int* sta
     if (!few && tiles[0] + tiles[1] > sms / 2) {
         if ((s = lay_out(prod, n, 256, 256, 128, dtype, &p)) != FP_OK) return s;
         p.late = late;
-        return launched(pairs(wide(0) || (n > 1 && wide(1))));
+        return launched(pairs(wide(prod[0]) || (n > 1 && wide(prod[1]))));
     }
     // one after the other, the second beside the first
     for (int i = 0; i < n; ++i) {
         p.late = late || i > 0;
-        p.run = wide(i) ? kRun : 0;
+        p.run = wide(prod[i]) ? kRun : 0;
         if (prod[i].swap) {
             const int bn = prod[i].J <= 16 ? 16 : prod[i].J <= 32 ? 32 : prod[i].J <= 64 ? 64 : 128;
             if ((s = lay_out(prod + i, 1, 128, bn, bn, dtype, &p)) != FP_OK) return s;
@@ -1156,26 +1216,14 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, int* sta
                          : bn == 64 ? launch_tiles<64>(p, splits, smem, st) : launch_tiles<128>(p, splits, smem, st));
         } else if (tiles[i] > sms / 2) {
             if ((s = lay_out(prod + i, 1, 256, 256, 128, dtype, &p)) != FP_OK) return s;
-            s = launched(pairs(wide(i)));
+            s = launched(pairs(wide(prod[i])));
         } else {
-            // The tile's width and the pairs that share it by the cycles that they are expected to take: the K blocks, the exchange of
-            // sums, finishing, and 3000 for everything else; a launch of more CTAs than run at once takes as many rounds.  Of
-            // two products each has its share of the SMs.
-            const int64_t kblocks = (prod[i].Kc + kBlockK - 1) / kBlockK;
-            const int64_t share = n > 1 && !few ? std::max<int64_t>(2, sms * tiles[i] * kblocks / work) : sms;
-            int bn = 256, S = 1;
-            double best = 0;
-            for (int b = 256; b >= 128; b /= 2)
-                for (int c = 1; c <= kMaxSplits && 2 * c <= std::max<int64_t>(kblocks, 2); ++c) {
-                    const int64_t ctas = 2 * c * ((prod[i].I + 255) / 256) * ((prod[i].J + b - 1) / b), room = std::min<int64_t>(share, split_room(c));
-                    const double cost = (double)((ctas + room - 1) / room) *
-                                        (3000 + (double)((kblocks + c - 1) / c) * (b == 256 ? 522 : 392) + 32.0 * b * (c - 1) / c + 11.0 * b / c);
-                    // (a 32-bit result whose runs would be longer than twice kRun: only where there is no other way)
-                    const double much = p.run && (kblocks + c - 1) / c > 2 * kRun * (512 / b) ? 1e6 * (b / 128) / c : 0;
-                    if (best == 0 || cost + much < best) { best = cost + much; bn = b; S = c; }
-                }
-            if ((s = lay_out(prod + i, 1, 256, bn, bn / 2, dtype, &p)) != FP_OK) return s;
-            s = launched(bn == 256 ? launch_split<256>(p, S, st) : launch_split<128>(p, S, st));
+            const int64_t extra = sums && i == n - 1 ? (sums->N + 127) / 128 : 0;
+            const SplitChoice c = split_choice(prod[i], share_of(prod, n, i, used), extra);
+            if ((s = lay_out(prod + i, 1, 256, c.bn, c.bn / 2, dtype, &p)) != FP_OK) return s;
+            used = c.ctas;
+            if (extra) { p.sums = *sums; p.sums.splits = 2 * c.S; p.sums_vec = sums_vec; }
+            s = launched(c.bn == 256 ? launch_split<256>(p, c.S, st) : launch_split<128>(p, c.S, st));
         }
         if (s != FP_OK) return s;
     }
@@ -1345,7 +1393,7 @@ extern "C" fp_status fp_linear_forward(const fp_linear_args* a, void* work, size
     e.y_type = a->y_dtype; e.pre_type = e.res_type = a->dtype; e.bias_type = a->bias_dtype; e.act = a->act; e.res_first = a->res_first;
     e.vec = aligned4(a->d_y, a->ld_y, a->y_dtype, a->M) && (!a->d_pre || aligned4(a->d_pre, a->ld_pre, a->dtype, a->M)) &&
             (!a->d_res || aligned4(a->d_res, a->ld_res, a->dtype, a->M));
-    return run_products(&p, 1, a->dtype, 0, status, st);
+    return run_products(&p, 1, a->dtype, 0, nullptr, 0, status, st);
 }
 
 extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work, size_t work_bytes, void* stream) {
@@ -1384,27 +1432,11 @@ extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work
         w += packed_bytes(a->M, a->N);
         dz = d.out[1]; ld_dz = d.ld_out[1];
     }
-    if (d.out[0] || d.out[1] || a->d_db) {
-        d.dy = static_cast<const uint16_t*>(a->d_dy); d.pre = static_cast<const uint16_t*>(a->d_pre); d.db = a->d_db;
-        d.ld_dy = a->ld_dy; d.ld_pre = a->ld_pre; d.M = a->M; d.N = (int)a->N; d.act = a->act; d.dtype = a->dtype; d.db_type = a->dw_dtype;
-        d.accumulate = a->accumulate;
-        const int64_t blocks = (a->N + 127) / 128;
-        d.splits = 1;
-        while (d.splits < 8 && a->M > 32 * d.splits && blocks * d.splits < 8 * sm_count()) d.splits *= 2;
-        const bool vec = (a->N & 7) == 0 && readable(a->d_dy, a->M, a->ld_dy) && (a->act == FP_ACT_NONE || readable(a->d_pre, a->M, a->ld_pre)) &&
-                         (!a->d_dz || readable(a->d_dz, a->M, a->ld_dz));
-        // fewer CTAs than SMs, and many rows: they are large (4637 x 15 unaligned 37 -> 19 us, 32768 x 1024 with gelu 164 -> 52)
-        const bool narrow = blocks * d.splits <= sm_count() && a->M > 64 * d.splits;
-        const DzKernel k = a->dtype == FP_DTYPE_BF16 ? dz_kernel<FP_DTYPE_BF16>(a->act, vec, narrow) : dz_kernel<FP_DTYPE_F16>(a->act, vec, narrow);
-        if ((s = launched(launch_clusters(k, d, blocks * d.splits, narrow ? 1024 : 256, 0, d.splits, st))) != FP_OK) return s;
-    }
-    if (!a->d_dx && !a->d_dw) return FP_OK;
     CopyJob jobs[2];
     int n_jobs = 0, n = 0;
     int64_t ld_x = a->ld_x, ld_w = a->ld_w;
     const void* x = a->d_dw ? place(a->d_x, a->M, a->K, &ld_x, &w, jobs, &n_jobs) : nullptr;
     const void* wt = a->d_dx ? place(a->d_w, a->N, a->K, &ld_w, &w, jobs, &n_jobs) : nullptr;
-    if (n_jobs && (s = copy_rows(jobs, n_jobs, st)) != FP_OK) return s;
     Product p[2];
     memset(p, 0, sizeof(p));
     if (a->d_dx) {
@@ -1425,9 +1457,30 @@ extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work
         if (a->accumulate) { r.e.res = a->d_dw; r.e.ld_res = a->ld_dw; r.e.res_type = a->dw_dtype; }
         r.e.vec = aligned4(a->d_dw, a->ld_dw, a->dw_dtype, a->N);
     }
-    // Where a launch in front of the products only sums dz's columns, they need not wait for it.
-    const int late = a->d_db && !d.out[0] && !d.out[1] && !n_jobs;
-    return run_products(p, n, a->dtype, late, status, st);
+    const bool writes = d.out[0] || d.out[1];
+    int along = 0, vec = 0;                              // whether the last product's launch sums dy's columns too (256 x 1000 x 2048: 12.7 -> 11.0 us)
+    if (writes || a->d_db) {
+        d.dy = static_cast<const uint16_t*>(a->d_dy); d.pre = static_cast<const uint16_t*>(a->d_pre); d.db = a->d_db;
+        d.ld_dy = a->ld_dy; d.ld_pre = a->ld_pre; d.M = a->M; d.N = (int)a->N; d.act = a->act; d.dtype = a->dtype; d.db_type = a->dw_dtype;
+        d.accumulate = a->accumulate;
+        vec = (a->N & 7) == 0 && readable(a->d_dy, a->M, a->ld_dy) && (a->act == FP_ACT_NONE || readable(a->d_pre, a->M, a->ld_pre)) &&
+              (!a->d_dz || readable(a->d_dz, a->M, a->ld_dz));
+        along = !writes && a->act == FP_ACT_NONE && room_for_sums(p, n, (a->N + 127) / 128);
+    }
+    if (writes || (a->d_db && !along)) {
+        const int64_t blocks = (a->N + 127) / 128;
+        d.splits = 1;
+        while (d.splits < 8 && a->M > 32 * d.splits && blocks * d.splits < 8 * sm_count()) d.splits *= 2;
+        // fewer CTAs than SMs, and many rows: they are large (4637 x 15 unaligned 37 -> 19 us, 32768 x 1024 with gelu 164 -> 52)
+        const bool narrow = blocks * d.splits <= sm_count() && a->M > 64 * d.splits;
+        const DzKernel k = a->dtype == FP_DTYPE_BF16 ? dz_kernel<FP_DTYPE_BF16>(a->act, vec, narrow) : dz_kernel<FP_DTYPE_F16>(a->act, vec, narrow);
+        if ((s = launched(launch_clusters(k, d, blocks * d.splits, narrow ? 1024 : 256, 0, d.splits, st))) != FP_OK) return s;
+    }
+    if (n_jobs && (s = copy_rows(jobs, n_jobs, st)) != FP_OK) return s;
+    if (!n) return FP_OK;
+    // Where the launch in front of the products only sums dz's columns, they need not wait for it.
+    const int late = a->d_db && !writes && !along && !n_jobs;
+    return run_products(p, n, a->dtype, late, along ? &d : nullptr, vec, status, st);
 }
 
 extern "C" fp_status fp_linear_status(int32_t* out) {

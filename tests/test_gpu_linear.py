@@ -370,6 +370,15 @@ def test_gradients_of_narrow_layers(B, M, N, K, act):
     backward_case(B, M, N, K, dtype=F16, act=act, out=F16, want="xwb")
 
 
+# Column sums by the last product's launch (no activation, few tiles) and by one of their own, on both sides of each limit.
+@pytest.mark.parametrize("M,N,K,pad", [(1, 300, 64, 0), (64, 1003, 520, 5), (129, 131, 200, 5), (256, 1000, 2048, 0), (300, 2048, 1000, 0), (2048, 264, 128, 0),
+                                       (2049, 264, 128, 0), (1500, 9000, 64, 0), (1500, 9600, 64, 0), (640, 128, 4096, 8)])
+@pytest.mark.parametrize("dtype,out", [(BF16, F32), (F16, F16), (BF16, BF16)])
+@pytest.mark.parametrize("want", ["xwb", "wb", "xb"])
+def test_column_sums_beside_the_products(B, M, N, K, pad, dtype, out, want):
+    backward_case(B, M, N, K, dtype=dtype, out=out, pad=pad, accumulate=want == "xwb", want=want)
+
+
 def test_calls_that_follow_each_other_share_their_scratch(B):
     """Twenty layers one after the other through one scratch buffer, each reading what the one before has written: launches that overlap
     keep their order."""
