@@ -1136,11 +1136,10 @@ int64_t tiles_of(const Product& r, int bn) { return ((r.I + 255) / 256) * ((r.J 
 // How linear_split_kernel takes a product that has `share` of the SMs: the tile's width and the pairs that share it by the cycles that they are
 // expected to take: the K blocks, the exchange of sums, finishing, and 3000 for everything else; a launch of more CTAs than run at once takes
 // as many rounds.  `extra`: clusters of the launch that sum columns.
-struct SplitChoice { int bn, S; int64_t ctas; bool fits; };
+struct SplitChoice { int bn, S; int64_t ctas; bool fits; double cycles; };
 SplitChoice split_choice(const Product& r, int64_t share, int64_t extra) {
     const int64_t kblocks = blocks_of(r);
-    SplitChoice best = {256, 1, 0, false};
-    double least = 0;
+    SplitChoice best = {256, 1, 0, false, 0};
     for (int b = 256; b >= 128; b /= 2)
         for (int c = 1; c <= kMaxSplits && 2 * c <= std::max<int64_t>(kblocks, 2); ++c) {
             const int64_t ctas = 2 * c * (tiles_of(r, b) + extra), room = std::min<int64_t>(share, split_room(c));
@@ -1148,16 +1147,37 @@ SplitChoice split_choice(const Product& r, int64_t share, int64_t extra) {
             const double much = wide(r) && (kblocks + c - 1) / c > 2 * kRun * (512 / b) ? 1e6 * (b / 128) / c : 0;
             const double cost = much + (double)((ctas + room - 1) / room) *
                                 (3000 + (double)((kblocks + c - 1) / c) * (b == 256 ? 522 : 392) + 32.0 * b * (c - 1) / c + 11.0 * b / c);
-            if (least == 0 || cost < least) { least = cost; best = {b, c, ctas, ctas <= room}; }
+            if (best.cycles == 0 || cost < best.cycles) best = {b, c, ctas, ctas <= room, cost};
         }
     return best;
 }
 
+// Cycles of linear_pair_kernel for a K block (2048 x 4096 x 4096: 66 us, with 32-bit results 97; 8192 x 4096 x 4096: 249 and 329).
+double pair_cycles(bool runs) { return runs ? 700 : 522; }
+
+// Whether a call's products go in one launch of linear_pair_kernel, where every pair takes its tiles one after the other, or in one each.  One
+// is for few tiles as much as a single product; two products of unlike sums take long together where a pair has one tile more of the
+// longer sum (8192 x 1024 x 1024, 128 tiles of 16 K blocks and 16 of 128: @@ us in one launch, @@ in two).
+bool together(const Product* prod, int n) {
+    const int64_t pairs = sm_count() / 2, t0 = tiles_of(prod[0], 256), t1 = n > 1 ? tiles_of(prod[1], 256) : 0;
+    if (prod[0].swap || t0 + t1 <= pairs) return false;
+    if (n < 2) return true;
+    int64_t longest = 0;
+    for (int64_t p = 0; p < pairs; ++p) {
+        const int64_t c0 = t0 > p ? (t0 - p - 1) / pairs + 1 : 0, c = t0 + t1 > p ? (t0 + t1 - p - 1) / pairs + 1 : 0;
+        longest = std::max(longest, c0 * blocks_of(prod[0]) + (c - c0) * blocks_of(prod[1]));
+    }
+    double apart = 0;
+    for (int i = 0; i < 2; ++i)
+        apart += (i ? t1 : t0) > pairs ? 3000 + pair_cycles(wide(prod[i])) * (((i ? t1 : t0) + pairs - 1) / pairs * blocks_of(prod[i])) : split_choice(prod[i], sm_count(), 0).cycles;
+    return 3000 + pair_cycles(wide(prod[0]) || wide(prod[1])) * longest <= apart;
+}
+
 // A call's products, one after the other, the second beside the first: the first has its share of the SMs by its work, the second what is
-// left, or its share.  (With few rows, where linear_tile_kernel takes the first, all of them.)
+// left, or its share.  (All of them where the first is one of few rows, for linear_tile_kernel, or one takes linear_pair_kernel.)
 int64_t share_of(const Product* prod, int n, int i, int64_t used) {
     const int sms = sm_count();
-    if (n < 2 || prod[0].swap) return sms;
+    if (n < 2 || prod[0].swap || tiles_of(prod[0], 256) + tiles_of(prod[1], 256) > sms / 2) return sms;
     const int64_t w0 = tiles_of(prod[0], 256) * blocks_of(prod[0]), w1 = tiles_of(prod[1], 256) * blocks_of(prod[1]);
     return std::max<int64_t>(i ? sms - used : 2, std::max<int64_t>(2, sms * (i ? w1 : w0) / (w0 + w1)));
 }
@@ -1166,11 +1186,12 @@ int64_t share_of(const Product* prod, int n, int i, int64_t used) {
 // (300 x 2048 x 1000, where they do not fit: 17.8 us with them, 13.3 with a launch in front).  With few rows the first product's CTAs are
 // short, and need not leave room (64 x 512 x 512 8.8 -> 6.9 us, 64 x 2048 x 1024 14.0 -> 9.8, 64 x 1000 x 2048 14.0 -> 14.9).
 bool room_for_sums(const Product* prod, int n, int64_t extra) {
-    if (n == 0 || prod[n - 1].swap) return false;
-    const bool few = prod[0].swap;
-    if ((few || n < 2 ? tiles_of(prod[n - 1], 256) : tiles_of(prod[0], 256) + tiles_of(prod[1], 256)) + extra > sm_count() / 2) return false;
-    const int64_t used = n > 1 && !few ? split_choice(prod[0], share_of(prod, n, 0, 0), 0).ctas : 0;
-    return split_choice(prod[n - 1], share_of(prod, n, n - 1, used), extra).fits;
+    if (n == 0 || prod[n - 1].swap || tiles_of(prod[n - 1], 256) + extra > sm_count() / 2 || together(prod, n)) return false;
+    const bool beside = n > 1 && !prod[0].swap && tiles_of(prod[0], 256) <= sm_count() / 2;
+    const int64_t used = beside ? split_choice(prod[0], share_of(prod, n, 0, 0), 0).ctas : 0;
+    const int64_t share = share_of(prod, n, n - 1, used);
+    const SplitChoice with = split_choice(prod[n - 1], share, extra);
+    return with.fits && with.cycles < split_choice(prod[n - 1], share, 0).cycles + 6000;       // (a launch's time)
 }
 
 // The products of a call (two, or one); `late`: their operands were there before the launch in front of them began; `sums`: column sums that the
@@ -1181,9 +1202,7 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, const Dz
     TileParams p;
     memset(&p, 0, sizeof(p));
     p.status = status; p.bf16 = dtype == FP_DTYPE_BF16;
-    const bool few = prod[0].swap;
-    int64_t tiles[2] = {0, 0}, used = 0;                 // tiles; CTAs of the first product
-    for (int i = 0; i < n; ++i) tiles[i] = tiles_of(prod[i], 256);
+    int64_t used = 0;                                    // CTAs of the first product
     auto pairs = [&](bool runs) -> cudaError_t {
         static std::atomic<unsigned long long> done[2];
         p.run = runs ? kRun : 0;
@@ -1192,7 +1211,7 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, const Dz
         return runs ? launch_clusters(linear_pair_kernel<true>, p, 2 * (sms / 2), PairShape<true>::kThreads, kAllSmem, 2, st)
                     : launch_clusters(linear_pair_kernel<false>, p, 2 * (sms / 2), PairShape<false>::kThreads, kAllSmem, 2, st);
     };
-    if (!few && tiles[0] + tiles[1] > sms / 2) {
+    if (together(prod, n)) {
         if ((s = lay_out(prod, n, 256, 256, 128, dtype, &p)) != FP_OK) return s;
         p.late = late;
         return launched(pairs(wide(prod[0]) || (n > 1 && wide(prod[1]))));
@@ -1214,7 +1233,7 @@ fp_status run_products(const Product* prod, int n, int dtype, int late, const Dz
             const int smem = splits > 1 ? kAllSmem : std::max(p.stages * stage, bn * 132 * 4) + 1024;
             s = launched(bn == 16 ? launch_tiles<16>(p, splits, smem, st) : bn == 32 ? launch_tiles<32>(p, splits, smem, st)
                          : bn == 64 ? launch_tiles<64>(p, splits, smem, st) : launch_tiles<128>(p, splits, smem, st));
-        } else if (tiles[i] > sms / 2) {
+        } else if (tiles_of(prod[i], 256) > sms / 2) {
             if ((s = lay_out(prod + i, 1, 256, 256, 128, dtype, &p)) != FP_OK) return s;
             s = launched(pairs(wide(prod[i])));
         } else {
