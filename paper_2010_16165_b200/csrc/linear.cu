@@ -1155,9 +1155,9 @@ SplitChoice split_choice(const Product& r, int64_t share, int64_t extra) {
 // Cycles of linear_pair_kernel for a K block (2048 x 4096 x 4096: 66 us, with 32-bit results 97; 8192 x 4096 x 4096: 249 and 329).
 double pair_cycles(bool runs) { return runs ? 700 : 522; }
 
-// Whether a call's products go in one launch of linear_pair_kernel, where every pair takes its tiles one after the other, or in one each.  One
-// is for few tiles as much as a single product; two products of unlike sums take long together where a pair has one tile more of the
-// longer sum (8192 x 1024 x 1024, 128 tiles of 16 K blocks and 16 of 128: @@ us in one launch, @@ in two).
+// Whether a call's products go in one launch of linear_pair_kernel, where every pair takes its tiles one after the other, or in one each.  The first
+// saves a launch and a last round of idle pairs; two products of unlike sums take long together where a pair has one tile more of the
+// longer sum (8192 x 1024 x 1024, 128 tiles of 16 K blocks and 16 of 128: 89 us in one launch, 53 in two).
 bool together(const Product* prod, int n) {
     const int64_t pairs = sm_count() / 2, t0 = tiles_of(prod[0], 256), t1 = n > 1 ? tiles_of(prod[1], 256) : 0;
     if (prod[0].swap || t0 + t1 <= pairs) return false;
@@ -1477,7 +1477,7 @@ extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work
         r.e.vec = aligned4(a->d_dw, a->ld_dw, a->dw_dtype, a->N);
     }
     const bool writes = d.out[0] || d.out[1];
-    int along = 0, vec = 0;                              // whether the last product's launch sums dy's columns too (256 x 1000 x 2048: 12.7 -> 11.0 us)
+    int along = 0, vec = 0;                              // whether the last product's launch sums dy's columns too (256 x 1000 x 2048: 12.7 -> 10.7 us)
     if (writes || a->d_db) {
         d.dy = static_cast<const uint16_t*>(a->d_dy); d.pre = static_cast<const uint16_t*>(a->d_pre); d.db = a->d_db;
         d.ld_dy = a->ld_dy; d.ld_pre = a->ld_pre; d.M = a->M; d.N = (int)a->N; d.act = a->act; d.dtype = a->dtype; d.db_type = a->dw_dtype;
