@@ -489,6 +489,8 @@ typedef void (*Kernel)(const LossParams);
 struct Choice { Kernel k; int threads, rows_a_block, cluster, smem; };
 
 constexpr int kMostUnits = 27;                           // a thread's units in shared memory: 216 KB a block
+constexpr int kOwnSmem = 1024;                           // at least what cross_entropy_kept_kernel has beside them
+static_assert(33 * sizeof(Part) <= kOwnSmem && kMostUnits * 512 * 16 + kOwnSmem <= 232448, "a block's shared memory");
 template <int DT>
 Choice choose(long long C, long long rows) {
     const int sms = sm_count();
@@ -550,7 +552,8 @@ extern "C" fp_status fp_cross_entropy(const fp_cross_entropy_args* a, void* stre
     cfg.blockDim = dim3((unsigned)c.threads);
     cfg.dynamicSmemBytes = (size_t)c.smem;
     cfg.stream = (cudaStream_t)stream;
-    if (c.smem > 48 * 1024 && cudaFuncSetAttribute((const void*)c.k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostUnits * 512 * 16) != cudaSuccess) {
+    // (A block has 48 KB without being asked for, of which the kernel's own shared memory is taken first.)
+    if (c.smem > 48 * 1024 - kOwnSmem && cudaFuncSetAttribute((const void*)c.k, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostUnits * 512 * 16) != cudaSuccess) {
         cudaGetLastError();
         return err(FP_ERR_CUDA, "fp_cross_entropy: no room for a row in shared memory");
     }
