@@ -45,12 +45,13 @@ __device__ __forceinline__ float exp2_of(float x) {
 constexpr float kLog2E = 1.4426950408889634f;
 __device__ __forceinline__ float exp_of(float d) { return exp2_of(d * kLog2E); }
 // e^(x - m) as 2^(x log2e - c) `fix`: c = m log2e rounded, and 2^(c - m log2e), which a fused product and sum gives exactly, makes up for
-// the rounding, however large m is.  Only where c might overflow (`far`) the difference is taken first.
+// the rounding.  That is at most 1/2 for |m| < 1e7 (c below 2^24); of larger m (`far`) the rounding alone would take one factor to 0
+// and the other to infinity, so the difference is taken first, whose own rounding is 2^-24 of it: exact where the exponential is not 0.
 struct Below {
     float m, c, fix;
     bool far;
     __device__ __forceinline__ explicit Below(float m_) : m(m_) {
-        far = !(fabsf(m) < 1e37f);
+        far = !(fabsf(m) < 1e7f);
         c = m * kLog2E;
         fix = far ? 1.0f : exp2_of(-fmaf(m, kLog2E, -c));
     }
