@@ -1,6 +1,6 @@
 // Softmax cross-entropy of every row and its gradient (fp_cross_entropy).
 //
-// With m the row's maximum, s = sum exp(x - m):  loss = log s - (1 - e) (x_y - m) - e (mean x - m),
+// With m the row's maximum, s = sum exp(x - m):  loss = log s + (m - x_y) - e mean(x - x_y),
 // d loss / dx_j = exp(x_j - m) / s - e / C - (1 - e) [j = y].
 //
 // Memory bound: logits are read once and the gradient written once.  The gradient needs s, so a row has to be kept between the
@@ -34,6 +34,7 @@ struct LossParams {
     long long ld_x, ld_dx, ignore, rows;
     int C, label_bytes;
     float smoothing, scale;
+    float unit, spread;                                  // of the smoothed mean: 2^-k with 2^k >= 4 C, and smoothing 2^k / C
 };
 
 // 2^x; results below 2^-126 are 0.
@@ -60,7 +61,7 @@ struct Below {
     __device__ __forceinline__ float value(float x) const { return far ? exp_of(x - m) : near_value(x) * fix; }
 };
 
-// Maximum, sum of exponentials below it, and plain sum of a part of a row.  A part of -inf alone has m = -inf, s = 0.
+// Maximum, sum of exponentials below it, and sum of `unit` (x - x_y) of a part of a row.  A part of -inf alone has m = -inf, s = 0.
 struct Part { float m, s, t; };
 __device__ __forceinline__ Part join(const Part& a, const Part& b) {
     Part r;
@@ -184,7 +185,9 @@ __device__ __forceinline__ Part join_all(Part a, Part* shared) {
     return a;
 }
 
-struct Row { long long label; float g, label_x; bool ignored, bad; };
+// `less`: what is taken from x `unit` to have `unit` (x - x_y), exactly but for one rounding and whatever the sizes.  (x itself summed loses what the row
+// has in common, 1e4 2^-24 for logits near 1e4, and overflows where two classes are masked by the lowest value.)
+struct Row { long long label; float g, label_x, less; bool ignored, bad; };
 template <int DT>
 __device__ __forceinline__ Row row_of(const LossParams& p, long long row) {
     Row r;
@@ -192,12 +195,14 @@ __device__ __forceinline__ Row row_of(const LossParams& p, long long row) {
     r.ignored = r.label == p.ignore;
     r.bad = !r.ignored && (r.label < 0 || r.label >= p.C);
     r.label_x = r.ignored || r.bad ? 0.0f : load1(p.x, row * p.ld_x + r.label, DT);
+    r.less = fabsf(r.label_x) < INFINITY ? -r.label_x * p.unit : 0.0f;      // (of a label's logit that is not finite, whatever makes it so is in the sum too)
     r.g = p.scale * (p.row_grad ? p.row_grad[row] : 1.0f);
     return r;
 }
 __device__ __forceinline__ float loss_of(const LossParams& p, const Row& r, const Part& a) {
-    float l = logf(a.s) - (1.0f - p.smoothing) * (r.label_x - a.m);
-    if (p.smoothing != 0.0f) l -= p.smoothing * (a.t / (float)p.C - a.m);
+    float l;
+    if (p.smoothing == 0.0f) l = logf(a.s) - (r.label_x - a.m);
+    else l = fmaf(2.0f, fmaf(-0.5f * p.spread, a.t, 0.5f * a.m - 0.5f * r.label_x), logf(a.s));        // (halves: the two may be as far apart as their type goes)
     return r.ignored ? 0.0f : r.bad ? NAN : l;
 }
 
@@ -260,7 +265,7 @@ __global__ void __launch_bounds__(256, 4) cross_entropy_kernel(const LossParams 
             if (k < used)
 #pragma unroll
                 for (int i = 0; i < E; ++i)
-                    if ((unsigned)((t + k * kStep) * E - shift + i) < (unsigned)p.C) a.t += U::get(u[k], i);
+                    if ((unsigned)((t + k * kStep) * E - shift + i) < (unsigned)p.C) a.t += fmaf(U::get(u[k], i), p.unit, r.less);
     a = join_all<G, 1>(a, shared);
     if (there && p.loss && t == 0) p.loss[row] = loss_of(p, r, a);
     if (there && p.dx) {
@@ -380,7 +385,7 @@ __global__ void __launch_bounds__(512, 3) cross_entropy_kept_kernel(const LossPa
             const bool whole = k >= lo && k < hi;
 #pragma unroll
             for (int i = 0; i < E; ++i)
-                if (whole || (unsigned)((t + k * kStep) * E - shift + i) < (unsigned)p.C) a.t += U::get(u, i);
+                if (whole || (unsigned)((t + k * kStep) * E - shift + i) < (unsigned)p.C) a.t += fmaf(U::get(u, i), p.unit, r.less);
         }
     a = join_all<G, CL>(a, shared);                      // (and all have read what dx may overwrite)
     if (p.loss && t == 0) p.loss[row] = loss_of(p, r, a);
@@ -465,7 +470,7 @@ __global__ void __launch_bounds__(1024) cross_entropy_twice_kernel(const LossPar
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             a.s += exp_of(x[u] - m0);
-            if (j + u * step < p.C) a.t += x[u];
+            if (j + u * step < p.C) a.t += fmaf(x[u], p.unit, r.less);
         }
     }
     a = join_all<1024, CL>(a, shared);                   // (and all have read the label's logit: dx may be x)
@@ -543,6 +548,9 @@ extern "C" fp_status fp_cross_entropy(const fp_cross_entropy_args* a, void* stre
     p.x = a->d_logits; p.labels = a->d_labels; p.row_grad = a->d_row_grad; p.loss = a->d_loss; p.dx = a->d_dlogits;
     p.ld_x = a->ld_logits; p.ld_dx = a->ld_dlogits; p.ignore = a->ignore_index; p.rows = a->rows; p.C = (int)a->classes; p.label_bytes = a->label_bytes;
     p.smoothing = a->label_smoothing; p.scale = a->grad_scale;
+    double all = 4.0;
+    while (all < 4.0 * (double)p.C) all *= 2.0;
+    p.unit = (float)(1.0 / all); p.spread = (float)((double)p.smoothing * all / (double)p.C);
     const Choice c = a->dtype == FP_DTYPE_F32 ? choose<FP_DTYPE_F32>(p.C, p.rows) : a->dtype == FP_DTYPE_BF16 ? choose<FP_DTYPE_BF16>(p.C, p.rows)
                                                                                                         : choose<FP_DTYPE_F16>(p.C, p.rows);
     const long long blocks = (a->rows + c.rows_a_block - 1) / c.rows_a_block * c.cluster;
