@@ -1342,15 +1342,16 @@ fp_status check(const fp_linear_grad_args* a) {
     return FP_OK;
 }
 
-// Whether the products need a dz of their own in scratch: where there is no tensor that they can read in place.
-bool dz_in_work(const fp_linear_grad_args* a) {
-    if (!a->d_dx && !a->d_dw) return false;
-    if (a->d_dz && readable(a->d_dz, a->M, a->ld_dz)) return false;
-    return a->act != FP_ACT_NONE || !readable(a->d_dy, a->M, a->ld_dy);
+// Where the products read dz: in d_dz, or without an activation in d_dy, if those can be read in place, or else in scratch.
+enum DzPlace { kDzNowhere, kDzOut, kDzIn, kDzWork };
+DzPlace dz_place(const fp_linear_grad_args* a) {
+    if (!a->d_dx && !a->d_dw) return kDzNowhere;
+    if (a->d_dz && readable(a->d_dz, a->M, a->ld_dz)) return kDzOut;
+    return a->act == FP_ACT_NONE && readable(a->d_dy, a->M, a->ld_dy) ? kDzIn : kDzWork;
 }
 size_t backward_work(const fp_linear_grad_args* a) {
     if (a->M == 0) return 0;
-    return (dz_in_work(a) ? packed_bytes(a->M, a->N) : 0) + (a->d_dw && !readable(a->d_x, a->M, a->ld_x) ? packed_bytes(a->M, a->K) : 0) +
+    return (dz_place(a) == kDzWork ? packed_bytes(a->M, a->N) : 0) + (a->d_dw && !readable(a->d_x, a->M, a->ld_x) ? packed_bytes(a->M, a->K) : 0) +
            (a->d_dx && !readable(a->d_w, a->N, a->ld_w) ? packed_bytes(a->N, a->K) : 0);
 }
 fp_status check_work(const void* work, size_t have, size_t need, Buffers& buf) {
@@ -1444,8 +1445,10 @@ extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work
     int64_t ld_dz = a->ld_dy;
     DzParams d;
     memset(&d, 0, sizeof(d));
-    if (a->d_dz) { d.out[0] = static_cast<uint16_t*>(a->d_dz); d.ld_out[0] = a->ld_dz; dz = a->d_dz; ld_dz = a->ld_dz; }
-    if (dz_in_work(a)) {
+    const DzPlace at = dz_place(a);
+    if (a->d_dz) { d.out[0] = static_cast<uint16_t*>(a->d_dz); d.ld_out[0] = a->ld_dz; }
+    if (at == kDzOut) { dz = a->d_dz; ld_dz = a->ld_dz; }
+    if (at == kDzWork) {
         d.out[1] = reinterpret_cast<uint16_t*>(w);
         d.ld_out[1] = (a->N + 7) / 8 * 8;
         w += packed_bytes(a->M, a->N);
