@@ -537,6 +537,10 @@ extern "C" fp_status fp_cross_entropy(const fp_cross_entropy_args* a, void* stre
     if ((((uintptr_t)a->d_logits | (uintptr_t)a->d_dlogits) & (uintptr_t)(bytes - 1)) || ((uintptr_t)a->d_labels & (uintptr_t)(a->label_bytes - 1)) ||
         (((uintptr_t)a->d_loss | (uintptr_t)a->d_row_grad) & 3))
         return err(FP_ERR_ARG, "fp_cross_entropy: a buffer is not aligned to its elements");
+    auto other = [](const void* out, const void* b) { return out && out == b; };
+    if (other(a->d_loss, a->d_logits) || other(a->d_loss, a->d_dlogits) || other(a->d_loss, a->d_labels) || other(a->d_loss, a->d_row_grad) ||
+        other(a->d_dlogits, a->d_labels) || other(a->d_dlogits, a->d_row_grad))
+        return err(FP_ERR_ARG, "fp_cross_entropy: an output is an input (only dlogits may be the logits) or the other output");
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, "fp_cross_entropy: no current device"); }
     Buffers buf(dev);

@@ -1,0 +1,33 @@
+"""Outputs of the training-step calls that are another buffer of the call are refused, before any GPU is asked; what the header allows is not."""
+import ctypes
+
+import pytest
+
+from paper_2010_16165_b200 import binding as B
+
+P = 1 << 20          # addresses that are never read
+X, W, Y, Z, A, C = (P * k for k in (2, 3, 4, 5, 6, 7))
+
+
+def refused(status):
+    """Whether a call was refused for such an output, and not for its addresses, which no GPU knows (or for the lack of one)."""
+    return status == B.FP_ERR_ARG and "output" in B.lib().fp_last_error().decode()
+
+
+def cross_entropy(**kw):
+    d = dict(rows=4, classes=8, dtype=B.FP_DTYPE_F32, label_bytes=4, ignore_index=-100, label_smoothing=0.0, grad_scale=1.0, d_logits=X, d_labels=W, d_row_grad=Y,
+             d_loss=Z, d_dlogits=A, ld_logits=8, ld_dlogits=8)
+    d.update(kw)
+    a = B.fp_cross_entropy_args(**d)
+    return B.lib().fp_cross_entropy(ctypes.addressof(a), None)
+
+
+@pytest.mark.parametrize("kw", [dict(d_loss=X), dict(d_loss=W), dict(d_loss=Y), dict(d_loss=A), dict(d_dlogits=W), dict(d_dlogits=Y),
+                                dict(d_loss=W, d_dlogits=None), dict(d_loss=None, d_dlogits=Y), dict(d_loss=X, d_dlogits=X)])
+def test_cross_entropy(kw):
+    assert refused(cross_entropy(**kw))
+
+
+@pytest.mark.parametrize("kw", [{}, dict(d_dlogits=X), dict(d_row_grad=None), dict(d_loss=None), dict(d_dlogits=None), dict(d_row_grad=None, d_loss=None), dict(d_labels=Y)])
+def test_cross_entropy_of_other_buffers(kw):
+    assert not refused(cross_entropy(**kw))
