@@ -1298,7 +1298,7 @@ fp_status check(const fp_linear_args* a) {
     const uintptr_t odd = (uintptr_t)a->d_x | (uintptr_t)a->d_w | (uintptr_t)a->d_res | (uintptr_t)a->d_pre;
     if ((odd & 1) || ((uintptr_t)a->d_y & (uintptr_t)(elem_bytes(a->y_dtype) - 1)) || ((uintptr_t)a->d_bias & (uintptr_t)(elem_bytes(a->bias_dtype) - 1)))
         return err(FP_ERR_ARG, "fp_linear_forward: a buffer is not aligned to its elements");
-    if (a->d_y == a->d_x || a->d_y == a->d_w || a->d_y == a->d_bias || (a->d_pre && (a->d_pre == a->d_x || a->d_pre == a->d_w || a->d_pre == a->d_y || a->d_pre == a->d_res)) ||
+    if (a->d_y == a->d_x || a->d_y == a->d_w || a->d_y == a->d_bias || (a->d_pre && (a->d_pre == a->d_x || a->d_pre == a->d_w || a->d_pre == a->d_y || a->d_pre == a->d_res || a->d_pre == a->d_bias)) ||
         (a->d_res == a->d_y && (a->y_dtype != a->dtype || (a->M > 1 && a->ld_res != a->ld_y))))
         return err(FP_ERR_ARG, "fp_linear_forward: an output is an input (only y may be res, with its type and row stride) or another output");
     return FP_OK;

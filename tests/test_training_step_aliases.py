@@ -31,3 +31,21 @@ def test_cross_entropy(kw):
 @pytest.mark.parametrize("kw", [{}, dict(d_dlogits=X), dict(d_row_grad=None), dict(d_loss=None), dict(d_dlogits=None), dict(d_row_grad=None, d_loss=None), dict(d_labels=Y)])
 def test_cross_entropy_of_other_buffers(kw):
     assert not refused(cross_entropy(**kw))
+
+
+def linear(**kw):
+    d = dict(M=4, N=8, K=16, dtype=B.FP_DTYPE_BF16, y_dtype=B.FP_DTYPE_BF16, bias_dtype=B.FP_DTYPE_BF16, act=0, res_first=0, reserved=0, d_x=X, d_w=W,
+             d_bias=A, d_res=Z, d_y=Y, d_pre=C, ld_x=16, ld_w=16, ld_res=8, ld_y=8, ld_pre=8)
+    d.update(kw)
+    a = B.fp_linear_args(**d)
+    return B.lib().fp_linear_forward(ctypes.addressof(a), None, 0, None)
+
+
+@pytest.mark.parametrize("kw", [dict(d_y=A), dict(d_pre=A), dict(d_pre=A, d_res=None), dict(d_pre=Z), dict(d_pre=Y)])
+def test_linear(kw):
+    assert refused(linear(**kw))
+
+
+@pytest.mark.parametrize("kw", [{}, dict(d_y=Z), dict(d_bias=None), dict(d_bias=None, d_pre=None), dict(d_bias=Z), dict(d_x=Z, d_w=Z, d_bias=Z)])
+def test_linear_of_other_buffers(kw):
+    assert not refused(linear(**kw))
