@@ -1354,6 +1354,12 @@ size_t backward_work(const fp_linear_grad_args* a) {
     return (dz_place(a) == kDzWork ? packed_bytes(a->M, a->N) : 0) + (a->d_dw && !readable(a->d_x, a->M, a->ld_x) ? packed_bytes(a->M, a->K) : 0) +
            (a->d_dx && !readable(a->d_w, a->N, a->ld_w) ? packed_bytes(a->N, a->K) : 0);
 }
+// (Inputs are copied into scratch, and dz is written there, before anything else is read or written.)
+fp_status check_work_apart(const void* work, size_t need, const void* const* others, int n) {
+    for (int i = 0; i < n && need && work; ++i)
+        if (work == others[i]) return err(FP_ERR_ARG, "fp_linear: the scratch is another buffer of the call");
+    return FP_OK;
+}
 fp_status check_work(const void* work, size_t have, size_t need, Buffers& buf) {
     if (need == 0) return FP_OK;
     if (!work || have < need) return err(FP_ERR_BOUNDS, "fp_linear: the scratch is smaller than the workspace call says");
@@ -1384,6 +1390,8 @@ extern "C" fp_status fp_linear_backward_workspace(const fp_linear_grad_args* a, 
 extern "C" fp_status fp_linear_forward(const fp_linear_args* a, void* work, size_t work_bytes, void* stream) {
     fp_status s = check(a);
     if (s != FP_OK || a->M == 0) return s;
+    const void* others[6] = {a->d_x, a->d_w, a->d_bias, a->d_res, a->d_y, a->d_pre};
+    if ((s = check_work_apart(work, forward_work(a), others, 6)) != FP_OK) return s;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, "fp_linear_forward: no current device"); }
     Buffers buf(dev);
@@ -1419,6 +1427,8 @@ extern "C" fp_status fp_linear_forward(const fp_linear_args* a, void* work, size
 extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work, size_t work_bytes, void* stream) {
     fp_status s = check(a);
     if (s != FP_OK) return s;
+    const void* others[8] = {a->d_dy, a->d_pre, a->d_x, a->d_w, a->d_dx, a->d_dw, a->d_db, a->d_dz};
+    if ((s = check_work_apart(work, backward_work(a), others, 8)) != FP_OK) return s;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, "fp_linear_backward: no current device"); }
     Buffers buf(dev);

@@ -49,3 +49,24 @@ def test_linear(kw):
 @pytest.mark.parametrize("kw", [{}, dict(d_y=Z), dict(d_bias=None), dict(d_bias=None, d_pre=None), dict(d_bias=Z), dict(d_x=Z, d_w=Z, d_bias=Z)])
 def test_linear_of_other_buffers(kw):
     assert not refused(linear(**kw))
+
+
+def scratch_refused(status):
+    return status == B.FP_ERR_ARG and "scratch is" in B.lib().fp_last_error().decode() and "another buffer" in B.lib().fp_last_error().decode()
+
+
+@pytest.mark.parametrize("work", [X, W, Y, Z, A, C])
+def test_scratch_of_linear(work):
+    """Rows 17 elements apart are copied into scratch, which is no other buffer of the call then; where none is needed it is not looked at."""
+    for ld, wanted in ((17, True), (16, False)):
+        a = B.fp_linear_args(M=4, N=8, K=16, dtype=B.FP_DTYPE_BF16, y_dtype=B.FP_DTYPE_BF16, bias_dtype=B.FP_DTYPE_BF16, act=0, res_first=0, reserved=0, d_x=X, d_w=W,
+                             d_bias=A, d_res=Z, d_y=Y, d_pre=C, ld_x=ld, ld_w=16, ld_res=8, ld_y=8, ld_pre=8)
+        assert scratch_refused(B.lib().fp_linear_forward(ctypes.addressof(a), work, 1 << 16, None)) == wanted
+
+
+@pytest.mark.parametrize("work", [X, W, Y, Z, A, C, 8 * P, 9 * P])
+def test_scratch_of_linear_gradients(work):
+    for ld, wanted in ((17, True), (16, False)):
+        a = B.fp_linear_grad_args(M=4, N=8, K=16, dtype=B.FP_DTYPE_BF16, dw_dtype=B.FP_DTYPE_F32, act=1, accumulate=0, d_dy=Y, d_pre=Z, d_x=X, d_w=W, d_dx=A, d_dw=C,
+                                  d_db=8 * P, d_dz=9 * P, ld_dy=8, ld_pre=8, ld_x=ld, ld_w=16, ld_dx=16, ld_dw=16, ld_dz=8)
+        assert scratch_refused(B.lib().fp_linear_backward(ctypes.addressof(a), work, 1 << 16, None)) == wanted
