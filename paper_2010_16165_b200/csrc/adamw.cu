@@ -350,6 +350,20 @@ const void* kernel_of(int pt, int gt, int bits) {
 bool dtype_ok(int d) { return d == FP_DTYPE_F32 || is_half(d); }
 bool multiple(const void* p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 
+// Whether something that a tensor's step writes is also something else of that tensor, or one of the step's device scalars.
+inline bool written_twice(const fp_adamw_tensor& t, const fp_adamw_hyper& h, bool device_scalars) {
+    const void *p = t.d_p, *m = t.d_m, *v = t.d_v, *g = t.d_g, *k = t.d_mask;        // (none of the first three is NULL)
+    if (p == m || p == v || p == g || p == k || m == v || m == g || m == k || v == g || v == k) return true;
+    if (t.state_bits == 32 && !device_scalars) return false;
+    auto in = [&](const void* s) { return s == p || s == m || s == v; };
+    const void *a = t.d_m_scale, *b = t.d_v_scale;
+    const bool scales = t.state_bits == 8;
+    if (scales && (in(a) || in(b) || a == b || a == g || a == k || b == g || b == k)) return true;
+    for (const void* s : {(const void*)h.d_lr, (const void*)h.d_grad_scale, (const void*)h.d_step})
+        if (s && (in(s) || (scales && (s == a || s == b)))) return true;
+    return false;
+}
+
 struct Kind { int p, g, bits; };
 inline bool is_of(const fp_adamw_tensor& x, const Kind& k) { return x.n > 0 && x.p_dtype == k.p && x.g_dtype == k.g && x.state_bits == k.bits; }
 
@@ -404,6 +418,8 @@ extern "C" fp_status fp_adamw_step(const fp_adamw_tensor* ts, int32_t count, con
         return err(FP_ERR_ARG, "fp_adamw_step: bad hyper-parameters (0 <= beta < 1, eps >= 0, step >= 1)");
     if (((uintptr_t)h->d_lr & 3) || ((uintptr_t)h->d_grad_scale & 3) || ((uintptr_t)h->d_step & 7))
         return err(FP_ERR_ARG, "fp_adamw_step: a device scalar is not aligned to its type");
+    const bool device_scalars = h->d_lr || h->d_grad_scale || h->d_step;
+    bool again = false;
     for (int i = 0; i < count; ++i) {
         const fp_adamw_tensor& t = ts[i];
         if (t.n < 0 || t.reserved) return err(FP_ERR_ARG, "fp_adamw_step: a tensor with a negative size, or reserved set");
@@ -418,7 +434,9 @@ extern "C" fp_status fp_adamw_step(const fp_adamw_tensor* ts, int32_t count, con
             (t.state_bits == 32 && (!multiple(t.d_m, 4) || !multiple(t.d_v, 4))) ||
             (t.state_bits == 8 && (!multiple(t.d_m_scale, 4) || !multiple(t.d_v_scale, 4))))
             return err(FP_ERR_ARG, "fp_adamw_step: a buffer is not aligned to its elements");
+        again = again || written_twice(t, *h, device_scalars);
     }
+    if (again) return err(FP_ERR_ARG, "fp_adamw_step: an output is another buffer of its tensor, or a device scalar");
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, "fp_adamw_step: no current device"); }
     Buffers buf(dev);

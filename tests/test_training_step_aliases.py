@@ -70,3 +70,26 @@ def test_scratch_of_linear_gradients(work):
         a = B.fp_linear_grad_args(M=4, N=8, K=16, dtype=B.FP_DTYPE_BF16, dw_dtype=B.FP_DTYPE_F32, act=1, accumulate=0, d_dy=Y, d_pre=Z, d_x=X, d_w=W, d_dx=A, d_dw=C,
                                   d_db=8 * P, d_dz=9 * P, ld_dy=8, ld_pre=8, ld_x=ld, ld_w=16, ld_dx=16, ld_dw=16, ld_dz=8)
         assert scratch_refused(B.lib().fp_linear_backward(ctypes.addressof(a), work, 1 << 16, None)) == wanted
+
+
+def adamw(hyper=None, **kw):
+    d = dict(n=64, per_row=8, p_dtype=0, g_dtype=0, state_bits=8, reserved=0, d_p=X, d_g=W, d_m=Y, d_v=Z, d_m_scale=A, d_v_scale=C, d_mask=8 * P)
+    d.update(kw)
+    ts = (B.fp_adamw_tensor * 2)(B.fp_adamw_tensor(n=64, p_dtype=0, g_dtype=0, state_bits=32, d_p=20 * P, d_g=21 * P, d_m=22 * P, d_v=23 * P), B.fp_adamw_tensor(**d))
+    h = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, grad_scale=1.0, step=1, d_lr=9 * P, d_grad_scale=10 * P, d_step=11 * P)
+    h.update(hyper or {})
+    h = B.fp_adamw_hyper(**h)
+    return B.lib().fp_adamw_step(ctypes.addressof(ts), 2, ctypes.addressof(h), None)
+
+
+@pytest.mark.parametrize("kw", [dict(d_g=X), dict(d_m=X), dict(d_v=X), dict(d_v=Y), dict(d_m=W), dict(d_m_scale=Z), dict(d_v_scale=A), dict(d_m_scale=W), dict(d_mask=X), dict(d_mask=C),
+                                dict(d_g=X, state_bits=32), dict(d_m=Z, state_bits=32), dict(d_mask=Y, state_bits=32),
+                                dict(hyper=dict(d_lr=X)), dict(hyper=dict(d_step=Z)), dict(hyper=dict(d_grad_scale=20 * P)), dict(hyper=dict(d_lr=C))])
+def test_adamw(kw):
+    assert refused(adamw(**kw))
+
+
+@pytest.mark.parametrize("kw", [{}, dict(d_mask=None), dict(d_mask=W), dict(d_m_scale=X, d_v_scale=X, state_bits=32), dict(n=0, d_g=X, d_m=X, d_v=X),
+                                dict(hyper=dict(d_lr=W, d_step=None, d_grad_scale=W)), dict(hyper=dict(d_lr=None, d_step=None, d_grad_scale=None))])
+def test_adamw_of_other_buffers(kw):
+    assert not refused(adamw(**kw))
