@@ -470,10 +470,12 @@ class AdamwTensors:
 def fp_adamw_tensors(tensors):
     """tensors: dicts of CUDA tensors - p (float32, bf16 or f16; updated), g, m, v (float32 like p's shape, or e4m3 codes: float8_e4m3fn
     or uint8 with float32 m_scale and v_scale, one for every FP_ADAMW_BLOCK elements) and optionally mask (uint8, one for every row of p,
-    or for every len / mask elements of a vector).  All contiguous.  Returns the table that fp_adamw_step takes."""
+    or for every len / mask elements of a vector).  All contiguous; what the step writes may be listed once.  Returns the table that
+    fp_adamw_step takes, made once for buffers that stay: a gradient that is allocated anew needs a new table."""
     import torch
     f8 = (torch.uint8, torch.float8_e4m3fn)
     arr = (fp_adamw_tensor * len(tensors))()
+    written, read = [], []
     for a, t in zip(arr, tensors):
         p, g, m, v, mask = t["p"], t["g"], t["m"], t["v"], t.get("mask")
         n, bits = p.numel(), 8 if m.dtype in f8 else 32
@@ -495,6 +497,12 @@ def fp_adamw_tensors(tensors):
         if bits == 8:
             a.d_m_scale, a.d_v_scale = t["m_scale"].data_ptr(), t["v_scale"].data_ptr()
         a.d_mask = mask.data_ptr() if per_row else None
+        if n:
+            written += [a.d_p, a.d_m, a.d_v] + ([a.d_m_scale, a.d_v_scale] if bits == 8 else [])
+            read += [a.d_g] + ([a.d_mask] if per_row else [])
+    once = set(written)
+    if len(once) != len(written) or not once.isdisjoint(read):
+        raise ValueError("a tensor that the step writes (p, m, v, m_scale or v_scale) is listed twice, or is another one's gradient or mask")
     return AdamwTensors(arr, [dict(t) for t in tensors])
 
 
