@@ -378,15 +378,27 @@ __global__ void __launch_bounds__(512, 3) cross_entropy_kept_kernel(const LossPa
             a.s = (lo + hi) * e.fix;
         }
     }
-    if (p.smoothing != 0.0f)
-#pragma unroll 1
-        for (int k = 0; k < count; ++k) {
+    if (p.smoothing != 0.0f) {
+        const Two unit = twice(p.unit), less = twice(r.less);
+        Two s = twice(0.0f);
+#pragma unroll 4
+        for (int k = lo; k < hi; ++k) {
             const uint4 u = mine[k * G];
-            const bool whole = k >= lo && k < hi;
+#pragma unroll
+            for (int i = 0; i < E; i += 2) s = add2(s, fma2(U::pair_at(u, i), unit, less));
+        }
+        float even, odd;
+        split(s, even, odd);
+        a.t = even + odd;
+        auto edge = [&](int k) {
+            const uint4 u = mine[k * G];
 #pragma unroll
             for (int i = 0; i < E; ++i)
-                if (whole || (unsigned)((t + k * kStep) * E - shift + i) < (unsigned)p.C) a.t += fmaf(U::get(u, i), p.unit, r.less);
-        }
+                if ((unsigned)((t + k * kStep) * E - shift + i) < (unsigned)p.C) a.t += fmaf(U::get(u, i), p.unit, r.less);
+        };
+        if (lo) edge(0);
+        if (hi < count) edge(hi);
+    }
     a = join_all<G, CL>(a, shared);                      // (and all have read what dx may overwrite)
     if (p.loss && t == 0) p.loss[row] = loss_of(p, r, a);
     if (p.dx) {
