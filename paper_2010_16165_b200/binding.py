@@ -79,7 +79,7 @@ fp_adamw_hyper = _struct("fp_adamw_hyper", a=(ctypes.c_double, "lr beta1 beta2 e
 
 
 # The same layouts for struct: a call's arguments are packed in a quarter of the time that a ctypes structure takes.
-_LINEAR, _LINEAR_GRAD, _CROSS_ENTROPY, _ADAMW_HYPER = (struct.Struct(f) for f in ("3q6i6P5q", "3q4i8P7q", "2q2iq2f5P2q", "6dq3P"))
+_LINEAR, _LINEAR_GRAD, _CROSS_ENTROPY, _ADAMW_TENSOR, _ADAMW_HYPER = (struct.Struct(f) for f in ("3q6i6P5q", "3q4i8P7q", "2q2iq2f5P2q", "2q4i7P", "6dq3P"))
 
 
 ALLOC_FN = ctypes.CFUNCTYPE(ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p)
@@ -474,9 +474,8 @@ def fp_adamw_tensors(tensors):
     fp_adamw_step takes, made once for buffers that stay: a gradient that is allocated anew needs a new table."""
     import torch
     f8 = (torch.uint8, torch.float8_e4m3fn)
-    arr = (fp_adamw_tensor * len(tensors))()
-    written, read = [], []
-    for a, t in zip(arr, tensors):
+    rows, written, read = [], [], []
+    for t in tensors:
         p, g, m, v, mask = t["p"], t["g"], t["m"], t["v"], t.get("mask")
         n, bits = p.numel(), 8 if m.dtype in f8 else 32
         blocks = -(-n // FP_ADAMW_BLOCK)
@@ -492,18 +491,21 @@ def fp_adamw_tensors(tensors):
             if mask.dtype != torch.uint8 or not mask.numel() or n % mask.numel():
                 raise ValueError("mask must be uint8, one entry for every row of p")
             per_row = n // mask.numel()
-        a.n, a.per_row, a.p_dtype, a.g_dtype, a.state_bits = n, per_row, _dtype(p, "p"), _dtype(g, "g"), bits
-        a.d_p, a.d_g, a.d_m, a.d_v = p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr()
+        out, into = [p.data_ptr(), m.data_ptr(), v.data_ptr()], [g.data_ptr()]
         if bits == 8:
-            a.d_m_scale, a.d_v_scale = t["m_scale"].data_ptr(), t["v_scale"].data_ptr()
-        a.d_mask = mask.data_ptr() if per_row else None
+            out += [t["m_scale"].data_ptr(), t["v_scale"].data_ptr()]
+        if per_row:
+            into.append(mask.data_ptr())
+        rows.append(_ADAMW_TENSOR.pack(n, per_row, _dtype(p, "p"), _dtype(g, "g"), bits, 0, out[0], into[0], out[1], out[2], *(out[3:] or (0, 0)),
+                                       into[1] if per_row else 0))
         if n:
-            written += [a.d_p, a.d_m, a.d_v] + ([a.d_m_scale, a.d_v_scale] if bits == 8 else [])
-            read += [a.d_g] + ([a.d_mask] if per_row else [])
+            written += out
+            read += into
     once = set(written)
     if len(once) != len(written) or not once.isdisjoint(read):
         raise ValueError("a tensor that the step writes (p, m, v, m_scale or v_scale) is listed twice, or is another one's gradient or mask")
-    return AdamwTensors(arr, [dict(t) for t in tensors])
+    array = (fp_adamw_tensor * len(rows)).from_buffer(bytearray(b"".join(rows))) if rows else (fp_adamw_tensor * 0)()
+    return AdamwTensors(array, [dict(t) for t in tensors])
 
 
 def fp_adamw_step(table, lr, step=1, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=1.0, d_lr=None, d_grad_scale=None,
