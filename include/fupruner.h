@@ -267,7 +267,7 @@ fp_status fp_query(fp_handle h, int32_t what, int32_t index, void* h_out, size_t
  * epoch's update can bring them back.  The masks of the epoch are kept (FP_Q_MASK / FP_Q_RANK); the graph
  * that fp_forward runs is NOT changed until fp_soft_prune_finish.
  *   d_updates   device fp32 or NULL.  Stands for "update the parameters W by using data X" (the library has no
- *               trainer): the concatenation, over the convolutions of the description in order (convolutions
+ *               gradients of convolutions): the concatenation, over the convolutions of the description in order (convolutions
  *               absorbed by aggressive fusion skipped), of one addend per weight of the fused bank,
  *               K_fused x C_fused x R x S each (FP_Q_CONV_BANK_ELEMS gives the count); W <- W + update, one
  *               fp32 addition per weight.
@@ -320,9 +320,10 @@ fp_status fp_rank_filters_static(const float* d_filters, int32_t K, int32_t per_
 /* ---- the training step around pruning ------------------------------------------------------
  *
  * Algorithm 1 prunes between the epochs of a training loop ("update the parameters W by using data X", line 2).  These
- * calls are that update for fully connected layers - the layer, its gradients, the loss they start from and the
- * optimizer step over all tensors - so that a program can retrain a pruned network beside fp_score / fp_prune /
- * fp_rank_filters_static without leaving the library.
+ * calls are that update for fully connected layers - the layer, its gradients, the loss they start from - and the
+ * optimizer step over the tensors of any network.  Stacks of such layers, and the classifier of a convolutional network, are
+ * retrained and pruned (fp_rank_filters_static) within the library; of convolutions and batch norms it has no gradients, and
+ * for those fp_adamw_step takes gradients from elsewhere.
  *
  * Conventions of these calls: they work on the caller's buffers and keep nothing; asynchronous on `stream` (NULL =
  * default stream); no allocation and no host synchronisation, so that they can be captured into a CUDA graph; every
@@ -330,7 +331,8 @@ fp_status fp_rank_filters_static(const float* d_filters, int32_t K, int32_t per_
  * device).  Matrices are row major; ld_* is the number of ELEMENTS from one row to the next, at least the row's length;
  * any alignment to the element's size is allowed.  Elements between a row's end and the next row are neither read
  * into a result nor written.  Outputs may not overlap inputs or each other unless a call says so (an output that IS
- * another buffer of the call is refused with FP_ERR_ARG; other overlaps are not looked for).  Make the first call of each
+ * another buffer of the call - of fp_adamw_step, of its tensor - is refused with FP_ERR_ARG; other overlaps are not looked
+ * for).  After FP_ERR_CUDA a part of the call may have been queued: its outputs are undefined.  Make the first call of each
  * kind on a device outside a capture: it loads code.
  */
 
@@ -363,7 +365,7 @@ typedef struct {
  * there is room for them) that are added with rounding: off by about 5e-7 then, by 1e-6 for every 1024 terms of a run otherwise.  Bias,
  * activation and residual are applied to the 32-bit sum, which is rounded once.  gelu's Phi is off by 1.5e-7 at most.  What is not finite
  * goes through by IEEE rules and stays in its row (x) or column (w, bias).  The order of sums depends on M, N, K, the types and the
- * GPU alone: the same call gives the same bits.
+ * GPU alone, not on alignment, bias, activation or residual: the same call gives the same bits.
  *   d_work, work_bytes   device scratch of at least fp_linear_workspace bytes, 256-byte aligned (NULL where that is 0).
  *               Two calls that may run at the same time need two; so do two captured graphs that may.
  * Errors: FP_ERR_ARG, FP_ERR_UNSUPPORTED (dtype), FP_ERR_BOUNDS (a size beyond 2^30, scratch too small), FP_ERR_CUDA.
@@ -393,7 +395,9 @@ typedef struct {
  *   dz = dy * act'(pre)      dx = dz w      dw = dz' x      db = sum of dz's rows
  * dz is computed in 32 bits; db sums it unrounded, the two products take it rounded to dtype.  Sums as in fp_linear_forward.
  * The derivative of relu at 0 is 0.  Scratch, streams and errors as in fp_linear_forward, with
- * fp_linear_backward_workspace.  At least one output must be given.
+ * fp_linear_backward_workspace.  At least one output must be given.  The same call gives the same bits; the order of the sums
+ * depends on M, N, K, the types and the GPU, and, because what is computed together shares the GPU, on which outputs are asked
+ * for, on the activation, and (db) on whether dy and dz lie at multiples of 16 bytes.
  */
 fp_status fp_linear_backward(const fp_linear_grad_args* args, void* d_work, size_t work_bytes, void* stream);
 
@@ -424,7 +428,8 @@ typedef struct {
 
 /*
  * fp_cross_entropy - softmax cross-entropy of every row, loss = -sum target log softmax(logits), and its gradient, in
- * one pass.  Sums and exponentials in 32 bits; exponentials below 2^-126 count as 0.  Logits of -inf have probability 0 (with smoothing they make the loss
+ * one pass.  Sums and exponentials in 32 bits; exponentials below 2^-126 count as 0.  Finite logits of any size give what the
+ * formula gives; the smoothed part is summed as differences from the label's logit, off by some 2^-23 of their mean size.  Logits of -inf have probability 0 (with smoothing they make the loss
  * infinite, as the formula does); a row that is -inf throughout, or holds NaN or +inf, gives NaN in that row alone; so does a
  * label outside [0, classes) other than ignore_index.  At least one of d_loss, d_dlogits.
  * Errors: FP_ERR_ARG, FP_ERR_UNSUPPORTED (dtype), FP_ERR_BOUNDS (rows or classes beyond 2^30), FP_ERR_CUDA.
@@ -467,7 +472,7 @@ typedef struct {
  * its exponent range (taken to 2^-22 of itself; v below 2^-126 counts as 0), and a positive one never becomes 0 (it takes the smallest code),
  * so that no step is divided by eps alone because of rounding.  The step itself uses m and v before they are rounded.
  * A gradient that is not finite makes its element's p, m and v not finite, and an infinite one the states of its block.
- *   h_tensors   host; read before the call returns.  No two tensors may overlap.
+ *   h_tensors   host; read before the call returns.  No two tensors may overlap (not looked for); gradients and masks may be shared.
  * Errors: FP_ERR_ARG, FP_ERR_UNSUPPORTED (dtype, state_bits), FP_ERR_BOUNDS (n beyond 2^40), FP_ERR_CUDA; they are found
  * before anything is launched, except FP_ERR_CUDA.
  */

@@ -444,8 +444,8 @@ __global__ void __launch_bounds__(kTileThreads) linear_tile_kernel(const __grid_
 // each and reads 32 KB.  Pairs are persistent; accumulators of two tiles fill tensor memory, so that a tile is finished by eight
 // warps while the next one is summed.  Warp 0 copies, warp 1 of the pair's first CTA issues the MMAs, warps 4-11 finish.
 // With RUNS the accumulators hold runs of a tile's sum instead (see kRun): sixteen warps add them up in registers.
-// What bounds it is L2: 32 KB a K block into every SM, 2.1 GB for 4096 x 8192 x 4096, at 11.8 TB/s; the tensor pipe is active for 74-78 %.
-// 8192 x 16384 x 4096 takes 876 us plain, 898-945 with gelu and a kept pre-activation (a library product 780-810).  Eight row tiles at a time over all column
+// What bounds it is L2: 32 KB a K block into every SM, 2.1 GB for 4096 x 8192 x 4096, in 190 us: 11.3 TB/s; the tensor pipe is active for 74-78 %.
+// 8192 x 16384 x 4096 takes 810-880 us plain, by card (10 TB/s), 820-945 with gelu and a kept pre-activation (a library product 780-810).  Eight row tiles at a time over all column
 // tiles keep what runs at once in L2: with 4, 6, 12, 16, 24 and 32 it took 5, 3, 1, 1, 5 and 11 % longer, with K ranges that begin
 // at different places in different pairs 5 %.
 
@@ -1135,7 +1135,8 @@ int64_t tiles_of(const Product& r, int bn) { return ((r.I + 255) / 256) * ((r.J 
 
 // How linear_split_kernel takes a product that has `share` of the SMs: the tile's width and the pairs that share it by the cycles that they are
 // expected to take: the K blocks, the exchange of sums, finishing, and 3000 for everything else; a launch of more CTAs than run at once takes
-// as many rounds.  `extra`: clusters of the launch that sum columns.
+// as many rounds.  `extra`: clusters of the launch that sum columns.  (The 3000 only weigh a round against longer sums: with 1000 or 9000 twelve
+// products from 200 x 300 x 1000 to 2048 x 2048 x 2048 took the same time to 1 %.)
 struct SplitChoice { int bn, S; int64_t ctas; bool fits; double cycles; };
 SplitChoice split_choice(const Product& r, int64_t share, int64_t extra) {
     const int64_t kblocks = blocks_of(r);
@@ -1152,7 +1153,9 @@ SplitChoice split_choice(const Product& r, int64_t share, int64_t extra) {
     return best;
 }
 
-// Cycles of linear_pair_kernel for a K block (2048 x 4096 x 4096: 66 us, with 32-bit results 97; 8192 x 4096 x 4096: 249 and 329).
+// What a K block costs in linear_pair_kernel, in split_choice's measure: as much as there where nothing but the copies into an SM bounds it, a third
+// more with 32-bit results (8192 x 4096 x 4096: 249 and 329 us where the rule was fitted, 191-213 and 309-347 on other cards).  It is the ratio that counts: at
+// these sizes all SMs copy at once, and a block takes about half a microsecond, twice that many cycles.
 double pair_cycles(bool runs) { return runs ? 700 : 522; }
 
 // Whether a call's products go in one launch of linear_pair_kernel, where every pair takes its tiles one after the other, or in one each.  The first
@@ -1191,7 +1194,9 @@ bool room_for_sums(const Product* prod, int n, int64_t extra) {
     const int64_t used = beside ? split_choice(prod[0], share_of(prod, n, 0, 0), 0).ctas : 0;
     const int64_t share = share_of(prod, n, n - 1, used);
     const SplitChoice with = split_choice(prod[n - 1], share, extra);
-    return with.fits && with.cycles < split_choice(prod[n - 1], share, 0).cycles + 6000;       // (a launch's time)
+    // (6000 is a launch's time.  With 0 256 x 1000 x 2048 took 11.9 us instead of 10.4, 1000 x 1000 x 1000 15.8 instead of 13.6, 64 x 512 x 512 7.8 instead of 6.7;
+    // with 20000 none of ten sizes changed.)
+    return with.fits && with.cycles < split_choice(prod[n - 1], share, 0).cycles + 6000;
 }
 
 // The products of a call (two, or one); `late`: their operands were there before the launch in front of them began; `sums`: column sums that the
@@ -1503,7 +1508,7 @@ extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work
         const int64_t blocks = (a->N + 127) / 128;
         d.splits = 1;
         while (d.splits < 8 && a->M > 32 * d.splits && blocks * d.splits < 8 * sm_count()) d.splits *= 2;
-        // fewer CTAs than SMs, and many rows: they are large (4637 x 15 unaligned 37 -> 19 us, 32768 x 1024 with gelu 164 -> 52)
+        // fewer CTAs than SMs, and many rows: they are large (4637 x 15 unaligned 37 -> 13-19 us, 32768 x 1024 with gelu 164 -> 68-85 with dz and db)
         const bool narrow = blocks * d.splits <= sm_count() && a->M > 64 * d.splits;
         const DzKernel k = a->dtype == FP_DTYPE_BF16 ? dz_kernel<FP_DTYPE_BF16>(a->act, vec, narrow) : dz_kernel<FP_DTYPE_F16>(a->act, vec, narrow);
         if ((s = launched(launch_clusters(k, d, blocks * d.splits, narrow ? 1024 : 256, 0, d.splits, st))) != FP_OK) return s;

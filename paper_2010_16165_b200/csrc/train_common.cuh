@@ -109,7 +109,7 @@ __device__ __forceinline__ Two inverse2(Two x) {
 
 // ---- activations ----------------------------------------------------------------------------------------------------
 // Two values at a time, in packed instructions: the epilogue of a product and dz are instruction-bound where the activation takes 40 instructions a
-// value (dz of 8192 x 16384 with gelu 174 us, of which the memory needs 123).
+// value (dz of 8192 x 16384 with gelu: 174 us one at a time, 143 two at a time, of which the memory needs 123).
 // tanh(u) = 1 - 2 / (1 + e^2u), so z/2 (1 + tanh u) = z / (1 + e^-2u): one exponential, and no cancellation where the result is
 // small.  e^-2u = inf gives z * 0, the limit.
 
