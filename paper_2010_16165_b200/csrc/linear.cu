@@ -1432,7 +1432,8 @@ extern "C" fp_status fp_linear_forward(const fp_linear_args* a, void* work, size
 extern "C" fp_status fp_linear_backward(const fp_linear_grad_args* a, void* work, size_t work_bytes, void* stream) {
     fp_status s = check(a);
     if (s != FP_OK) return s;
-    const void* others[8] = {a->d_dy, a->d_pre, a->d_x, a->d_w, a->d_dx, a->d_dw, a->d_db, a->d_dz};
+    const void* others[8] = {a->d_dy, a->act != FP_ACT_NONE ? a->d_pre : nullptr, a->d_dw ? a->d_x : nullptr, a->d_dx ? a->d_w : nullptr,      // (what is not read may be anything)
+                             a->d_dx, a->d_dw, a->d_db, a->d_dz};
     if ((s = check_work_apart(work, backward_work(a), others, 8)) != FP_OK) return s;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return err(FP_ERR_CUDA, "fp_linear_backward: no current device"); }

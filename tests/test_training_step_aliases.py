@@ -72,6 +72,15 @@ def test_scratch_of_linear_gradients(work):
         assert scratch_refused(B.lib().fp_linear_backward(ctypes.addressof(a), work, 1 << 16, None)) == wanted
 
 
+@pytest.mark.parametrize("kw,work", [(dict(act=0), Z), (dict(d_dw=None), X), (dict(d_dx=None), W)])
+def test_scratch_in_place_of_what_is_not_read(kw, work):
+    d = dict(M=4, N=8, K=16, dtype=B.FP_DTYPE_BF16, dw_dtype=B.FP_DTYPE_F32, act=1, accumulate=0, d_dy=Y, d_pre=Z, d_x=X, d_w=W, d_dx=A, d_dw=C,
+             d_db=8 * P, d_dz=None, ld_dy=9, ld_pre=8, ld_x=16, ld_w=16, ld_dx=16, ld_dw=16, ld_dz=8)
+    d.update(kw)
+    a = B.fp_linear_grad_args(**d)
+    assert not scratch_refused(B.lib().fp_linear_backward(ctypes.addressof(a), work, 1 << 16, None))
+
+
 def adamw(hyper=None, **kw):
     d = dict(n=64, per_row=8, p_dtype=0, g_dtype=0, state_bits=8, reserved=0, d_p=X, d_g=W, d_m=Y, d_v=Z, d_m_scale=A, d_v_scale=C, d_mask=8 * P)
     d.update(kw)
